@@ -375,6 +375,88 @@ lipz_status lipz_set_gemm_timing(lipz_grid* g, int32_t enable);
 lipz_status lipz_gemm_timing(lipz_grid* g, double* h_ms, int64_t* h_launches, double* h_flops,
                              double* h_bytes);
 
+/* ---- residual-block operators ----
+ *
+ * The layers of a pre-norm residual block, h' = h + act(norm(h) W + b), for a
+ * batch of cells that each own their parameters: forward, gradients, and with
+ * 8-bit operands.  They need no grid handle.
+ *
+ * A matrix is a lipz_mat: element (c, i, j) of cell c at p[c * cell + i * ld + j],
+ * strides in elements.  Columns are contiguous; ld >= columns, ld <= 2^20,
+ * cell >= 0, at most 65535 cells.  Inputs may share storage between cells (cell = 0); an output's
+ * cells may not overlap each other, nor an output an input, except where a
+ * call says so.  p needs the alignment of its elements only (16-byte aligned rows
+ * run faster).  Vectors (float*) are contiguous in a cell and `_cell` floats
+ * apart between cells.  An optional matrix is left out with p = NULL.
+ *
+ * Element types: LIPZ_F32, LIPZ_BF16, LIPZ_F16; LIPZ_FP8 is OCP e4m3 (largest
+ * value 448, no infinities).  Sums, norms and activations are formed in fp32
+ * and rounded to nearest even once, on the store.  A value beyond the output
+ * type's range becomes an infinity (LIPZ_FP8: see below); NaN stays NaN.
+ *
+ * Every call takes an argument struct (abi_version = LIPZ_ABI_VERSION), the
+ * workspace (device memory, 256-byte aligned, at least the bytes that the
+ * call's lipz_*_workspace_bytes returns for the same struct; 0 means the
+ * struct is invalid; its contents need not be kept between calls, and one
+ * workspace may serve calls on one stream), and the hipStream_t it runs on.
+ * Calls check their arguments on the host, enqueue and return; they neither
+ * allocate nor synchronise, and may be captured into a graph.  Results do not
+ * depend on what else runs: sums are taken in a fixed order.  rows = 0 is
+ * allowed (gradients of parameters are then 0).  Errors: LIPZ_E_INVAL,
+ * LIPZ_E_WORKSPACE, LIPZ_E_UNSUPPORTED (sizes beyond the limits named at the
+ * call) before anything is enqueued, LIPZ_E_HIP. */
+enum { LIPZ_F32 = 0, LIPZ_BF16 = 1, LIPZ_F16 = 2, LIPZ_FP8 = 3 };
+/* Activations of these operators, beside LIPZ_ACT_LINEAR .. LIPZ_ACT_TANH:
+ * GELU z Phi(z) (Phi the normal distribution function), SiLU z / (1 + e^-z). */
+enum { LIPZ_ACT_GELU = 4, LIPZ_ACT_SILU = 5 };
+#define LIPZ_MAX_LD ((int64_t)1 << 20)
+
+typedef struct {
+  void* p;
+  int64_t ld, cell;
+} lipz_mat;
+
+/* Root-mean-square norm with the residual's addition:
+ *   h = x + residual;  rstd[i] = 1 / sqrt(mean_j h^2 + eps);
+ *   y = h * rstd * gamma
+ * h is rounded to dtype for its store only: rstd and y come from the fp32 sum.
+ * y_dtype: dtype, or LIPZ_FP8 with a scale per row,
+ *   y_scale[i] = max(max_j |h rstd gamma| / 448, 2^-126),  y = e4m3(h rstd gamma / y_scale);
+ * a row that holds a NaN or an infinity then has the scale NaN and only NaN in
+ * y.  residual, h and rstd may be NULL; h may be x or residual itself (same p,
+ * ld and cell).  rows >= 0, 1 <= cols <= 2^20, eps > 0. */
+typedef struct {
+  int32_t abi_version, dtype, y_dtype, cells, rows, cols;
+  float eps;
+  lipz_mat x, residual, h, y;
+  const float* gamma;   /* [cells][cols] */
+  int64_t gamma_cell;
+  float* rstd;          /* [cells][rows], dense; may be NULL */
+  float* y_scale;       /* [cells][rows], dense; LIPZ_FP8 only */
+} lipz_rms_norm_args;
+size_t lipz_rms_norm_workspace_bytes(const lipz_rms_norm_args* a);
+lipz_status lipz_rms_norm(const lipz_rms_norm_args* a, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients, from the stored h and rstd and the gradient dy of y:
+ *   u = dy * gamma;  xh = h * rstd;
+ *   dx = rstd (u - xh mean_j(u xh)) + dh;  dgamma[j] = sum_i dy xh
+ * dh: the gradient that reaches h from elsewhere (the skip connection), may be
+ * NULL.  dx is the gradient of x and of residual alike; it may be dy or dh
+ * itself.  dgamma may be NULL, and is per cell: where cells share gamma, its
+ * gradient is the sum over them. */
+typedef struct {
+  int32_t abi_version, dtype, cells, rows, cols;
+  lipz_mat h, dy, dh, dx;
+  const float* gamma;
+  int64_t gamma_cell;
+  const float* rstd;    /* [cells][rows], dense */
+  float* dgamma;        /* [cells][cols] */
+  int64_t dgamma_cell;
+} lipz_rms_norm_backward_args;
+size_t lipz_rms_norm_backward_workspace_bytes(const lipz_rms_norm_backward_args* a);
+lipz_status lipz_rms_norm_backward(const lipz_rms_norm_backward_args* a, void* d_workspace, size_t workspace_bytes,
+                                   void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

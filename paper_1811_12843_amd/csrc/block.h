@@ -1,0 +1,216 @@
+// Shared by the residual-block operators (norm.hip, linear.hip, linear_fp8.hip):
+// element types, wide loads and stores at any alignment, activations, and the
+// host's checks of matrices.
+#pragma once
+
+#include <type_traits>
+
+#include "lipz_internal.h"
+
+namespace lipz {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+// ---- element types ----
+// __bf16 and _Float16 convert from fp32 with one rounding to nearest even.
+
+template <class T>
+struct Vec8;
+template <>
+struct Vec8<float> {
+  typedef float type __attribute__((ext_vector_type(8)));
+};
+template <>
+struct Vec8<__bf16> {
+  typedef __bf16 type __attribute__((ext_vector_type(8)));
+};
+template <>
+struct Vec8<_Float16> {
+  typedef _Float16 type __attribute__((ext_vector_type(8)));
+};
+
+// Eight elements in a row at the alignment of one: the hardware takes wide
+// global accesses at any address; 16-byte aligned ones run faster.
+template <class T>
+struct __attribute__((packed, aligned(sizeof(T)))) Eight {
+  typename Vec8<T>::type v;
+};
+
+// Elements 0 .. min(n, 8) - 1 at p as fp32, the rest 0.
+template <class T>
+__device__ __forceinline__ f32x8 load8(const T* p, int n) {
+  if (n >= 8) return __builtin_convertvector(reinterpret_cast<const LIPZ_GLOBAL Eight<T>*>((const LIPZ_GLOBAL T*)p)->v, f32x8);
+  f32x8 r = {};
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) r[e] = (float)as_global(p)[e];
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store8(T* p, int n, f32x8 v) {
+  const typename Vec8<T>::type w = __builtin_convertvector(v, typename Vec8<T>::type);
+  if (n >= 8) {
+    reinterpret_cast<LIPZ_GLOBAL Eight<T>*>((LIPZ_GLOBAL T*)p)->v = w;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) as_global(p)[e] = w[e];
+}
+
+// e4m3: NaN stays NaN; callers scale so that nothing exceeds 448 by more than a rounding.
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+struct __attribute__((packed, aligned(1))) EightBytes {
+  u32x2 v;
+};
+__device__ __forceinline__ u32x2 to_fp8(f32x8 v) {
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
+  return u32x2{(unsigned)lo, (unsigned)hi};
+}
+__device__ __forceinline__ void store8_fp8(uint8_t* p, int n, f32x8 v) {
+  const u32x2 w = to_fp8(v);
+  if (n >= 8) {
+    reinterpret_cast<LIPZ_GLOBAL EightBytes*>((LIPZ_GLOBAL uint8_t*)p)->v = w;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) as_global(p)[e] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+}
+
+constexpr float kFp8Max = 448.f;
+constexpr float kFp8MinScale = 1.17549435e-38f;  // 2^-126: its reciprocal and the quotients by it are finite
+
+// max that keeps a NaN of either side
+__device__ __forceinline__ float max_nan(float a, float b) { return (a > b || a != a) ? a : b; }
+// The scale of a row of largest magnitude m >= 0, infinite or NaN: NaN for the last two.
+__device__ __forceinline__ float fp8_scale(float m) {
+  const float s = m / kFp8Max;
+  return s < __builtin_inff() ? (s < kFp8MinScale ? kFp8MinScale : s) : __builtin_nanf("");
+}
+
+// ---- activations: z -> act(z), and act'(z) ----
+// FAST: for outputs that are rounded to 16 bits.  erf by Abramowitz and
+// Stegun 7.1.26 (absolute error 1.5e-7), exponentials and reciprocals of the
+// hardware's 1 ulp; else the library's functions.
+
+constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
+
+template <bool FAST>
+__device__ __forceinline__ float exp_of(float x) {
+  return FAST ? __builtin_amdgcn_exp2f(x * 1.44269504088896341f) : expf(x);
+}
+template <bool FAST>
+__device__ __forceinline__ float recip(float x) {
+  return FAST ? __builtin_amdgcn_rcpf(x) : 1.f / x;
+}
+// Phi(z); with FAST e must be e^(-z^2 / 2)
+template <bool FAST>
+__device__ __forceinline__ float normal_cdf(float z, float e) {
+  if (!FAST) return 0.5f * (1.f + erff(z * kInvSqrt2));
+  const float x = __builtin_fabsf(z) * kInvSqrt2;
+  const float t = recip<true>(fmaf(0.3275911f, x, 1.f));
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float q = 0.5f * p * t * e;  // Phi(-|z|)
+  return z < 0.f ? q : 1.f - q;
+}
+template <bool FAST>
+__device__ __forceinline__ float tanh_of(float z) {
+  if (!FAST) return tanhf(z);
+  const float z2 = z * z;
+  const float small = z * fmaf(z2, fmaf(z2, fmaf(z2, -0.05396825397f, 0.13333333333f), -0.33333333333f), 1.f);
+  const float big = fmaf(-2.f, recip<true>(1.f + exp_of<true>(2.f * z)), 1.f);
+  return z2 < 0.0625f ? small : big;
+}
+
+template <bool FAST>
+__device__ __forceinline__ float act_of(int act, float z, float slope) {
+  switch (act) {
+    case LIPZ_ACT_RELU: return z < 0.f ? 0.f : z;
+    case LIPZ_ACT_LRELU: return z < 0.f ? slope * z : z;
+    case LIPZ_ACT_TANH: return tanh_of<FAST>(z);
+    case LIPZ_ACT_GELU: return z * normal_cdf<FAST>(z, FAST ? exp_of<true>(-0.5f * z * z) : 0.f);
+    case LIPZ_ACT_SILU: return z * recip<FAST>(1.f + exp_of<FAST>(-z));
+    default: return z;
+  }
+}
+template <bool FAST>
+__device__ __forceinline__ float act_slope(int act, float z, float slope) {
+  switch (act) {
+    case LIPZ_ACT_RELU: return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
+    case LIPZ_ACT_LRELU: return z > 0.f ? 1.f : (z <= 0.f ? slope : z);
+    case LIPZ_ACT_TANH: {
+      const float t = tanh_of<FAST>(z);
+      return fmaf(-t, t, 1.f);
+    }
+    case LIPZ_ACT_GELU: {
+      const float e = exp_of<FAST>(-0.5f * z * z);
+      return fmaf(z * kInvSqrt2Pi, e, normal_cdf<FAST>(z, e));
+    }
+    case LIPZ_ACT_SILU: {
+      const float s = recip<FAST>(1.f + exp_of<FAST>(-z));
+      return s * fmaf(z, 1.f - s, 1.f);
+    }
+    default: return 1.f;
+  }
+}
+
+// ---- sums over the lanes of a wave, in a fixed order ----
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) v += __shfl_xor(v, s, 64);
+  return v;
+}
+__device__ __forceinline__ float wave_max_nan(float v) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) v = max_nan(v, __shfl_xor(v, s, 64));
+  return v;
+}
+
+// ---- the host's checks ----
+
+constexpr int64_t kMaxWide = 1 << 20;  // columns of a matrix
+constexpr int kMaxCells = 65535;       // a grid's second dimension
+
+inline int elem_size(int dtype) { return dtype == LIPZ_F32 ? 4 : dtype == LIPZ_FP8 ? 1 : 2; }
+inline bool valid_float(int dtype) { return dtype == LIPZ_F32 || dtype == LIPZ_BF16 || dtype == LIPZ_F16; }
+
+// Strides and alignment of a [cells][rows][cols] matrix.  `out`: written, so
+// its cells must lie apart.
+inline lipz_status check_mat(const lipz_mat& m, int cells, int64_t rows, int64_t cols, int dtype, bool out) {
+  if (m.ld < cols || m.cell < 0) return LIPZ_E_INVAL;
+  if (m.ld > LIPZ_MAX_LD) return LIPZ_E_UNSUPPORTED;
+  if ((uintptr_t)m.p % (size_t)elem_size(dtype)) return LIPZ_E_INVAL;
+  if (m.cell > (INT64_MAX / 16) / cells) return LIPZ_E_INVAL;
+  if (out && cells > 1 && rows > 0) {
+    // cells one after the other, or side by side inside the rows
+    const bool apart = m.cell >= (rows - 1) * m.ld + cols;
+    const bool beside = m.cell >= cols && (int64_t)(cells - 1) * m.cell + cols <= m.ld;
+    if (!apart && !beside) return LIPZ_E_INVAL;
+  }
+  return LIPZ_OK;
+}
+inline lipz_status check_vec(const float* p, int64_t cell, int cells, int64_t cols, bool out) {
+  if ((uintptr_t)p % 4 || cell < 0 || cell > (INT64_MAX / 16) / cells) return LIPZ_E_INVAL;
+  return out && cells > 1 && cell < cols ? LIPZ_E_INVAL : LIPZ_OK;
+}
+inline bool same_mat(const lipz_mat& a, const lipz_mat& b) { return a.p == b.p && a.ld == b.ld && a.cell == b.cell; }
+
+inline lipz_status check_workspace(const void* p, size_t have, size_t need) {
+  if (!need) return LIPZ_E_INVAL;
+  return !p || ((uintptr_t)p & 255) || have < need ? LIPZ_E_WORKSPACE : LIPZ_OK;
+}
+// out[c][j] = sum over n rows of part[c][n][cols] (norm.hip)
+hipError_t launch_sum_parts(const float* part, int n, int cols, int cells, float* out, int64_t out_cell, hipStream_t s);
+
+inline lipz_status launched() { return hipGetLastError() == hipSuccess ? LIPZ_OK : LIPZ_E_HIP; }
+
+}  // namespace lipz

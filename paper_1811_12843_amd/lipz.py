@@ -23,6 +23,9 @@ LOSSES = {"bce": LIPZ_LOSS_BCE, "wasserstein": LIPZ_LOSS_WASSERSTEIN}
 LIPZ_TRAINER_GRADIENT, LIPZ_TRAINER_NES, LIPZ_TRAINER_ES = 0, 1, 2
 LIPZ_STATIC_WORKSPACE_BYTES = 64 << 20
 TRAINERS = {"gradient": LIPZ_TRAINER_GRADIENT, "nes": LIPZ_TRAINER_NES, "es": LIPZ_TRAINER_ES}
+LIPZ_F32, LIPZ_BF16, LIPZ_F16, LIPZ_FP8 = 0, 1, 2, 3
+LIPZ_ACT_GELU, LIPZ_ACT_SILU = 4, 5
+LIPZ_MAX_LD = 1 << 20
 ACTS = {"linear": LIPZ_ACT_LINEAR, "relu": LIPZ_ACT_RELU, "lrelu": LIPZ_ACT_LRELU, "tanh": LIPZ_ACT_TANH}
 
 _i32, _i64, _f32, _u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_uint64
@@ -91,6 +94,32 @@ def config_from_dict(d):
     return c
 
 
+class lipz_mat(ctypes.Structure):
+    """Element (c, i, j) at p[c * cell + i * ld + j]; lipz_mat() is a matrix left out."""
+    _fields_ = [("p", _vp), ("ld", _i64), ("cell", _i64)]
+
+
+class _Args(ctypes.Structure):
+    """Arguments of a residual-block operator, by the names of the C struct; abi_version is set."""
+
+    def __init__(self, **kw):
+        super().__init__(LIPZ_ABI_VERSION, **kw)
+
+
+def _args(name, ints, rest):
+    fields = [(f, _i32) for f in ["abi_version"] + ints.split()]
+    kinds = {"f": _f32, "m": lipz_mat, "p": _vp, "l": _i64}
+    fields += [(f, kinds[k]) for k, f in (r.split(":") for r in rest.split())]
+    return type(name, (_Args,), {"_fields_": fields, "__module__": __name__})
+
+
+lipz_rms_norm_args = _args("lipz_rms_norm_args", "dtype y_dtype cells rows cols",
+                           "f:eps m:x m:residual m:h m:y p:gamma l:gamma_cell p:rstd p:y_scale")
+lipz_rms_norm_backward_args = _args("lipz_rms_norm_backward_args", "dtype cells rows cols",
+                                    "m:h m:dy m:dh m:dx p:gamma l:gamma_cell p:rstd p:dgamma l:dgamma_cell")
+#LINEAR_ARGS
+_BLOCK = {c.__name__[:-5]: c for c in (lipz_rms_norm_args, lipz_rms_norm_backward_args)}
+
 _SIGS = {
     "lipz_workspace_bytes": (_sz, [ctypes.POINTER(lipz_config), _i64]),
     "lipz_grid_create": (_i32, [ctypes.POINTER(lipz_config), _vp, _sz, _vp, _i64, _vp,
@@ -125,6 +154,10 @@ _SIGS = {
     "lipz_test_es_select": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _i64, _i64, _f32]),
     "lipz_test_tile_map": (_i32, [_i32, _vp, _i32, _vp]),
 }
+
+for _n, _c in _BLOCK.items():
+    _SIGS[_n] = (_i32, [ctypes.POINTER(_c), _vp, _sz, _vp])
+    _SIGS[_n + "_workspace_bytes"] = (_sz, [ctypes.POINTER(_c)])
 
 _lib = None
 
@@ -283,6 +316,26 @@ def lipz_gemm_timing(g):
                                            ctypes.byref(by)),
            "lipz_gemm_timing", g)
     return ms.value, n.value, fl.value, by.value
+
+
+# Residual-block operators: each takes its argument struct, the workspace and the stream.
+
+def lipz_rms_norm_workspace_bytes(args):
+    return load_library().lipz_rms_norm_workspace_bytes(ctypes.byref(args))
+
+
+def lipz_rms_norm(args, d_workspace, workspace_bytes, stream):
+    return _check(load_library().lipz_rms_norm(ctypes.byref(args), d_workspace, workspace_bytes, stream),
+                  "lipz_rms_norm")
+
+
+def lipz_rms_norm_backward_workspace_bytes(args):
+    return load_library().lipz_rms_norm_backward_workspace_bytes(ctypes.byref(args))
+
+
+def lipz_rms_norm_backward(args, d_workspace, workspace_bytes, stream):
+    return _check(load_library().lipz_rms_norm_backward(ctypes.byref(args), d_workspace, workspace_bytes, stream),
+                  "lipz_rms_norm_backward")
 
 
 def lipz_test_gemm(stream, d_desc, M, N, K, d_A, lda, a_trans, ones_row, d_B, ldb, b_trans, d_C, ldc,

@@ -1,0 +1,53 @@
+"""What the tests of the residual-block operators share: padded inputs, guarded outputs, calls and comparisons."""
+import numpy as np
+import torch
+
+import paper_1811_12843_amd as L
+
+# name: torch type, the library's, explicit bits of the significand, smallest normal exponent
+TYPES = {"f32": (torch.float32, L.LIPZ_F32, 23, -126), "bf16": (torch.bfloat16, L.LIPZ_BF16, 7, -126),
+         "f16": (torch.float16, L.LIPZ_F16, 10, -14), "fp8": (torch.float8_e4m3fn, L.LIPZ_FP8, 3, -6)}
+
+
+def half_ulp(v, kind):
+    """Half a unit in the last place of the values v (float64) in a type: what one correct rounding may be off."""
+    _, _, bits, low = TYPES[kind]
+    return np.exp2(np.maximum(np.frexp(v)[1] - 1.0, low) - bits - 1)
+
+
+def mat(t):
+    return L.lipz_mat() if t is None else L.lipz_mat(t.data_ptr(), t.stride(1), t.stride(0))
+
+
+def padded(g, cells, rows, cols, dtype, pad, scale=1.0, off=0):
+    """[cells][rows][cols] inside a larger allocation whose other elements are NaN."""
+    big = torch.full((cells * (rows * (cols + pad) + 3) + off + 8,), float("nan"), dtype=dtype, device="cuda")
+    t = big[off:off + cells * (rows * (cols + pad) + 3)].view(cells, -1)[:, :rows * (cols + pad)]
+    t = t.as_strided((cells, rows, cols), (t.stride(0), cols + pad, 1), big.storage_offset() + off)
+    t.copy_((torch.randn(cells, rows, cols, generator=g, device="cuda") * scale).to(dtype))
+    return t
+
+
+def blank(cells, rows, cols, dtype, pad=0):
+    """An output with `pad` guard columns, all of it 7; and a check that the guards still are."""
+    big = torch.full((cells, rows, cols + pad), 7.0, device="cuda").to(dtype)
+    return big[:, :, :cols], lambda: bool((big[:, :, cols:].float() == 7.0).all())
+
+
+def call(name, args):
+    nb = getattr(L, name + "_workspace_bytes")(args)
+    ws = torch.full((nb,), 0xFF, dtype=torch.uint8, device="cuda")  # NaNs wherever it is read unwritten
+    getattr(L, name)(args, ws.data_ptr(), nb, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+
+
+def close(got, want, kind, floor, what):
+    """|got - want| <= half a unit in the last place of the type + floor; NaN and infinities in the same places."""
+    got, want = got.double().cpu().numpy(), want.double().cpu().numpy()
+    floor = floor.double().cpu().numpy() if isinstance(floor, torch.Tensor) else floor
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    ok = np.isfinite(want)
+    assert np.array_equal(got[~ok & ~np.isnan(want)], want[~ok & ~np.isnan(want)]), what
+    floor = np.broadcast_to(floor, want.shape)[ok]
+    off = np.abs(got[ok] - want[ok]) - (half_ulp(want[ok], kind) + floor)
+    assert off.size == 0 or off.max() <= 0, (what, float(off.max()))

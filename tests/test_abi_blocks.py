@@ -1,0 +1,97 @@
+"""CPU checks of the residual-block operators' ABI: struct layouts against the C compiler, workspace sizing, and every
+refusal that the header names (all of them on the host: nothing here launches a kernel)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+import paper_1811_12843_amd as L
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 20  # a placeholder address, 256-byte aligned
+
+
+def mat(cols, rows=4, p=P, ld=None, cell=None):
+    ld = cols if ld is None else ld
+    return L.lipz_mat(p, ld, rows * ld if cell is None else cell)
+
+
+def norm(**kw):
+    d = dict(dtype=L.LIPZ_BF16, y_dtype=L.LIPZ_BF16, cells=2, rows=4, cols=24, eps=1e-5, x=mat(24), residual=mat(24),
+             h=mat(24), y=mat(24), gamma=P, gamma_cell=24, rstd=P, y_scale=P)
+    return L.lipz_rms_norm_args(**dict(d, **kw))
+
+
+def norm_bwd(**kw):
+    d = dict(dtype=L.LIPZ_BF16, cells=2, rows=4, cols=24, h=mat(24), dy=mat(24), dh=mat(24), dx=mat(24), gamma=P,
+             gamma_cell=24, rstd=P, dgamma=P, dgamma_cell=24)
+    return L.lipz_rms_norm_backward_args(**dict(d, **kw))
+
+
+NONE = L.lipz_mat()
+BAD = {
+    "lipz_rms_norm": (norm, [
+        dict(dtype=3), dict(dtype=-1), dict(y_dtype=L.LIPZ_F32), dict(cells=0), dict(rows=-1), dict(cols=0), dict(eps=0.0),
+        dict(eps=float("nan")), dict(eps=float("inf")), dict(x=NONE), dict(y=NONE), dict(gamma=None),
+        dict(y_dtype=L.LIPZ_FP8, y_scale=None), dict(x=mat(24, ld=23)), dict(y=mat(24, cell=-1)), dict(x=mat(24, p=P + 1)),
+        dict(y=mat(24, cell=95)), dict(h=mat(24, cell=0)), dict(gamma=P + 2), dict(rstd=P + 2), dict(gamma_cell=-24)], [
+        dict(cols=(1 << 20) + 1, x=mat((1 << 20) + 1), residual=NONE, h=NONE, y=mat((1 << 20) + 1)),
+        dict(x=mat(24, ld=(1 << 20) + 8)), dict(cells=65536)]),
+    "lipz_rms_norm_backward": (norm_bwd, [
+        dict(dtype=3), dict(cells=0), dict(rows=-1), dict(cols=0), dict(h=NONE), dict(dy=NONE), dict(dx=NONE),
+        dict(gamma=None), dict(rstd=None), dict(rstd=P + 1), dict(dy=mat(24, ld=8)), dict(dx=mat(24, cell=24)),
+        dict(dgamma_cell=23), dict(dgamma=P + 1)], [
+        dict(dh=mat(24, ld=(1 << 20) + 8)), dict(cells=65536)]),
+}
+
+
+@pytest.mark.parametrize("name", sorted(BAD))
+def test_refusals(name):
+    make, bad, unsupported = BAD[name]
+    fn, need = getattr(L, name), getattr(L, name + "_workspace_bytes")
+    nb = need(make())
+    assert nb > 0 and nb % 256 == 0
+    for kws, status in ((bad, L.LIPZ_E_INVAL), (unsupported, L.LIPZ_E_UNSUPPORTED)):
+        for kw in kws:
+            a = make(**kw)
+            assert need(a) == 0, kw
+            with pytest.raises(L.LipzError) as e:
+                fn(a, P, 1 << 40, None)
+            assert e.value.status == status, kw
+    a = make()
+    a.abi_version = 99
+    assert need(a) == 0
+    for p, n in ((None, nb), (P + 128, nb), (P, nb - 1)):
+        with pytest.raises(L.LipzError) as e:
+            fn(make(), p, n, None)
+        assert e.value.status == L.LIPZ_E_WORKSPACE
+    lib = L.load_library()
+    assert getattr(lib, name)(None, P, nb, None) == L.LIPZ_E_INVAL
+    assert getattr(lib, name + "_workspace_bytes")(None) == 0
+
+
+@pytest.mark.parametrize("name", sorted(BAD))
+def test_cells_inside_rows_and_shared_inputs_are_taken(name):
+    make, need = BAD[name][0], getattr(L, name + "_workspace_bytes")
+    side = lambda: L.lipz_mat(P, 48, 24)  # noqa: E731  two cells side by side in a row
+    kw = dict(y=side(), x=side()) if name == "lipz_rms_norm" else dict(dx=side(), dy=side())
+    assert need(make(**kw)) > 0
+    kw = dict(x=mat(24, cell=0), gamma_cell=0) if name == "lipz_rms_norm" else dict(h=mat(24, cell=0), gamma_cell=0)
+    assert need(make(**kw)) > 0
+
+
+@pytest.mark.parametrize("name", ["lipz_mat"] + [n + "_args" for n in sorted(BAD)])
+def test_struct_layout_matches_c(name, tmp_path):
+    cls = getattr(L, name)
+    fields = [f for f, _ in cls._fields_]
+    src = ['#include <stdio.h>', '#include <stddef.h>', '#include "lipz.h"', "int main(void) {",
+           f'printf("%zu\\n", sizeof({name}));']
+    src += [f'printf("%zu\\n", offsetof({name}, {f}));' for f in fields]
+    (tmp_path / "t.c").write_text("\n".join(src + ["return 0; }"]))
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), str(tmp_path / "t.c"), "-o", str(tmp_path / "t")],
+                   check=True)
+    out = [int(x) for x in subprocess.run([str(tmp_path / "t")], capture_output=True, text=True,
+                                          check=True).stdout.split()]
+    assert out[0] == ctypes.sizeof(cls)
+    assert out[1:] == [getattr(cls, f).offset for f in fields]
