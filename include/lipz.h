@@ -457,6 +457,73 @@ size_t lipz_rms_norm_backward_workspace_bytes(const lipz_rms_norm_backward_args*
 lipz_status lipz_rms_norm_backward(const lipz_rms_norm_backward_args* a, void* d_workspace, size_t workspace_bytes,
                                    void* hip_stream);
 
+/* Matrix product with bias, activation and residual:
+ *   z = x w + bias;  pre = z;  y = act(z) + residual
+ * x [rows][fan_in], w [fan_in][fan_out] (the layout of lipz_param_layout).
+ * bias, residual and pre may be NULL; pre is what lipz_linear_backward wants.
+ * y may be residual itself.  slope: LIPZ_ACT_LRELU's, > 0.  Of these products
+ * and lipz_quantize_weights alike: 1 <= fan_in, fan_out <= 2^20, rows <= 2^21,
+ * and each output at most 2^24 blocks of 64 x 64 over all cells. */
+typedef struct {
+  int32_t abi_version, dtype, cells, rows, fan_in, fan_out, act;
+  float slope;
+  lipz_mat x, w, residual, pre, y;
+  const float* bias;    /* [cells][fan_out] */
+  int64_t bias_cell;
+} lipz_linear_args;
+size_t lipz_linear_workspace_bytes(const lipz_linear_args* a);
+lipz_status lipz_linear(const lipz_linear_args* a, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients, from dy of y (which is also the residual's gradient):
+ *   dz = dy * act'(pre);  dx = dz w^T;  dw = x^T dz;  db[j] = sum_i dz
+ * pre is not read with LIPZ_ACT_LINEAR (may be NULL there).  relu' and
+ * lrelu' at 0 are those of z < 0.  dx (then w may be NULL), dw (then x may be
+ * NULL) and db may be NULL, not all three.  With 16-bit types the products
+ * take dz rounded to dtype; db sums it unrounded.  dw and db are per cell:
+ * where cells share w or bias, their gradients are the sums over them. */
+typedef struct {
+  int32_t abi_version, dtype, cells, rows, fan_in, fan_out, act;
+  float slope;
+  lipz_mat x, w, pre, dy, dx, dw;
+  float* db;            /* [cells][fan_out] */
+  int64_t db_cell;
+} lipz_linear_backward_args;
+size_t lipz_linear_backward_workspace_bytes(const lipz_linear_backward_args* a);
+lipz_status lipz_linear_backward(const lipz_linear_backward_args* a, void* d_workspace, size_t workspace_bytes,
+                                 void* hip_stream);
+
+/* Weights for lipz_linear_fp8: column j of w [fan_in][fan_out] becomes row j
+ * of q [fan_out][fan_in] (LIPZ_FP8) with
+ *   scale[j] = max(max_k |w[k][j]| / 448, 2^-126),  q[j][k] = e4m3(w[k][j] / scale[j]);
+ * a column that holds a NaN or an infinity has the scale NaN and only NaN. */
+typedef struct {
+  int32_t abi_version, dtype, cells, fan_in, fan_out;
+  lipz_mat w, q;
+  float* scale;         /* [cells][fan_out] */
+  int64_t scale_cell;
+} lipz_quantize_weights_args;
+size_t lipz_quantize_weights_workspace_bytes(const lipz_quantize_weights_args* a);
+lipz_status lipz_quantize_weights(const lipz_quantize_weights_args* a, void* d_workspace, size_t workspace_bytes,
+                                  void* hip_stream);
+
+/* The product of lipz_linear on e4m3 operands:
+ *   z = x_scale[i] w_scale[j] sum_k x[i][k] w[j][k] + bias;  y = act(z) + residual
+ * x [rows][fan_in] as lipz_rms_norm writes it, w [fan_out][fan_in] as
+ * lipz_quantize_weights does; residual and y of y_dtype (not LIPZ_FP8). */
+typedef struct {
+  int32_t abi_version, y_dtype, cells, rows, fan_in, fan_out, act;
+  float slope;
+  lipz_mat x, w, residual, y;
+  const float* x_scale; /* [cells][rows] */
+  int64_t x_scale_cell;
+  const float* w_scale; /* [cells][fan_out] */
+  int64_t w_scale_cell;
+  const float* bias;    /* [cells][fan_out] */
+  int64_t bias_cell;
+} lipz_linear_fp8_args;
+size_t lipz_linear_fp8_workspace_bytes(const lipz_linear_fp8_args* a);
+lipz_status lipz_linear_fp8(const lipz_linear_fp8_args* a, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -179,6 +179,7 @@ __device__ __forceinline__ float wave_max_nan(float v) {
 
 constexpr int64_t kMaxWide = 1 << 20;  // columns of a matrix
 constexpr int kMaxCells = 65535;       // a grid's second dimension
+constexpr int kMaxRows = 1 << 21;      // rows of a product, in blocks of 64 a grid's second dimension
 
 inline int elem_size(int dtype) { return dtype == LIPZ_F32 ? 4 : dtype == LIPZ_FP8 ? 1 : 2; }
 inline bool valid_float(int dtype) { return dtype == LIPZ_F32 || dtype == LIPZ_BF16 || dtype == LIPZ_F16; }
@@ -202,7 +203,11 @@ inline lipz_status check_vec(const float* p, int64_t cell, int cells, int64_t co
   if ((uintptr_t)p % 4 || cell < 0 || cell > (INT64_MAX / 16) / cells) return LIPZ_E_INVAL;
   return out && cells > 1 && cell < cols ? LIPZ_E_INVAL : LIPZ_OK;
 }
-inline bool same_mat(const lipz_mat& a, const lipz_mat& b) { return a.p == b.p && a.ld == b.ld && a.cell == b.cell; }
+// A product's workgroups (64 x 64 outputs at least, 512 splits in all at most) and the
+// threads that join its splits stay far below 2^31.
+inline lipz_status check_tiles(int64_t rows, int64_t cols, int64_t cells) {
+  return ((rows + 63) / 64) * ((cols + 63) / 64) * cells > (1 << 24) ? LIPZ_E_UNSUPPORTED : LIPZ_OK;
+}
 
 inline lipz_status check_workspace(const void* p, size_t have, size_t need) {
   if (!need) return LIPZ_E_INVAL;

@@ -1,0 +1,600 @@
+// The matrix product behind lipz_linear, lipz_linear_backward and
+// lipz_linear_fp8: out = epilogue(A B) for every cell, on the matrix cores.
+//
+//   out(i, j) = sum_k A(i, k) B(k, j),  0 <= i < M, 0 <= j < N, 0 <= k < K
+//
+// An operand is KC (k contiguous: A [M][K] or B stored [N][K]) or KM (k is the
+// row: A stored [K][M], B [K][N]).
+//
+// A workgroup owns a BM x BN tile and walks K in slices of 128 bytes per row
+// (32 k of fp32, 64 of 16 bits, 128 of e4m3) through two LDS stages.  A slice is
+// multiplied in two parts: the second part's fragments are read before the
+// first one's MFMAs, the next slice's first ones before the second's, and the
+// slice after the next is asked for as soon as every wave holds the present
+// one in registers; one barrier per slice.
+//
+// LDS.  KC: a row of 128 bytes is eight 16-byte chunks, chunk c at place
+// c ^ (row % 8), so that the 16 rows that a fragment read touches lie on all
+// banks.  KM: rows of the tile's columns; the chunk index is xored with bits
+// of k (km_swizzle), so that the k rows that a transposing read (16 bits) or
+// four b32 reads (fp32) touch lie on different banks.  Lanes permute the
+// global chunk they fetch, not the LDS address: loads go straight into LDS.
+//
+// Loads: buffer_load ... lds, 16 bytes a lane.  What lies past an operand is
+// zeros in LDS, by the resource's extent or, at the end of K, by an offset past
+// it.  That takes KC rows of whole chunks, and rows that begin and end on 4
+// bytes; other operands are copied into such rows first (pack_kernel).
+//
+// MFMAs take the B fragment first, so that a lane ends up with four columns
+// of a row; the tile then passes through LDS and is finished and stored in
+// rows of 8 elements per lane.
+#pragma once
+
+#include "block.h"
+
+namespace lipz {
+
+// The operand types of e4m3 products, by how they are formed.  The e4m3 MFMAs
+// (16 x 16 x 32 and, at twice the rate, 16 x 16 x 128) align their products to the
+// largest before they add them: measured on normal operands, both give sums that
+// are 1.4e-5 off in the 2-norm, at most 1.2e-5 (K = 128), 3.2e-6 (1024), 1.0e-6
+// (8192) of the sum of magnitudes.  Fp8Wide takes the second.  Fp8 turns the
+// fragments into f16, which holds every e4m3 value, and multiplies at fp32 accuracy.
+struct Fp8 {};
+struct Fp8Wide {};
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void lds_any;
+
+template <class E>
+struct ElemSize {
+  static constexpr int value = sizeof(E);
+};
+template <>
+struct ElemSize<Fp8> {
+  static constexpr int value = 1;
+};
+template <>
+struct ElemSize<Fp8Wide> {
+  static constexpr int value = 1;
+};
+
+// How a product's outputs are finished.
+struct Finish {
+  void *y, *pre;
+  const void* r;
+  int64_t y_ld, y_cell, pre_ld, pre_cell, r_ld, r_cell, bias_cell, xs_cell, ws_cell;  // in elements
+  const float *bias, *xs, *ws;  // xs, ws: scales of rows and columns (e4m3)
+  int act;
+  float slope;
+};
+
+struct GemmArgs {
+  const char *A, *B;
+  int64_t a_ld, a_cell, b_ld, b_cell;  // in bytes
+  int M, N, K;
+  int tiles_m, tiles_n, cells, splits, per_split;  // per_split: slices of a split
+  float* part;                                     // splits > 1: sums [split][cell][M][part_ld]
+  int part_ld;
+  Finish f;
+};
+
+constexpr int kSlice = 128;  // bytes of a row in a slice
+constexpr uint32_t kPast = 0x80000000u;
+
+// ---- finishing: 8 columns of a row from column n on, `left` of them inside ----
+template <class T>
+__device__ __forceinline__ void finish8(const Finish& f, int c, int m, int n, int left, f32x8 v, const f32x8& bias,
+                                        const f32x8& ws) {
+  constexpr bool FAST = sizeof(T) < 4;
+  if (f.xs) {
+    const float xs = as_global(f.xs)[c * f.xs_cell + m];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= xs * ws[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] += bias[e];
+  if (f.pre) store8((T*)f.pre + c * f.pre_cell + m * f.pre_ld + n, left, v);
+  if (f.act != LIPZ_ACT_LINEAR) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act_of<FAST>(f.act, v[e], f.slope);
+  }
+  if (f.r) {
+    const f32x8 r = load8((const T*)f.r + c * f.r_cell + m * f.r_ld + n, left);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += r[e];
+  }
+  store8((T*)f.y + c * f.y_cell + m * f.y_ld + n, left, v);
+}
+__device__ __forceinline__ f32x8 column8(const float* p, int64_t cell, int c, int n, int left) {
+  return p && left > 0 ? load8(p + c * cell + n, left) : f32x8{};
+}
+
+// ---- operands ----
+
+// The place of chunk x (16 bytes) of k row k in a KM tile of R columns is
+// x ^ km_swizzle(k).  16 bits: a transposing read takes 32 bytes of each of
+// the k rows 8 g + 0 .. 3 (or 4 .. 7), g the lane's group of 16; two groups
+// are served at a time.  fp32: a read takes 64 bytes of k rows 4 g + u.
+template <int ES, int R>
+__device__ __forceinline__ int km_swizzle(int k) {
+  if (ES == 4) return 4 * ((k >> 2) & 3);
+  if (R * ES >= 256) return 2 * ((k & 3) | ((k >> 1) & 4));
+  return 2 * (((k >> 1) & 1) | ((k >> 2) & 2));
+}
+
+template <int ES, bool KC, int R, int NT>
+struct Operand {
+  static constexpr int EPC = 16 / ES, BKE = kSlice / ES;
+  static constexpr int NI = R * 8 / NT;             // chunks of a slice per thread
+  static constexpr int CPR = KC ? 8 : R * ES / 16;  // chunks of an LDS row
+  const char* base;  // the next slice of the tile
+  int64_t step;      // bytes per slice
+  int extent;        // KC: bytes from base to the end of the tile's last row; KM: bytes of the operand's columns from the tile's on
+  int ld;            // KM: row pitch
+  int kleft;         // k left from the next slice on
+  uint32_t off[NI];  // the thread's chunks, from base
+  int k;             // KC: first k of the thread's chunks in their slice (the same in all of them)
+
+  __device__ __forceinline__ void init(const char* p, int64_t ld_bytes, int rc0, int rc_all, int K, int k0) {
+    ld = (int)ld_bytes;
+    kleft = K - k0;
+    if (KC) {
+      base = p + (int64_t)rc0 * ld_bytes + (int64_t)k0 * ES;
+      step = kSlice;
+      extent = (min(rc_all - rc0, R) - 1) * ld + (kleft * ES + 15) / 16 * 16;  // (packed rows end in zeros)
+    } else {
+      base = p + (int64_t)k0 * ld_bytes + (int64_t)rc0 * ES;
+      step = BKE * ld_bytes;
+      extent = ((rc_all - rc0) * ES + 3) / 4 * 4;
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int q = i * NT + (int)threadIdx.x, row = q / CPR, at = q % CPR;
+      const int x = KC ? at ^ (row & 7) : at ^ km_swizzle<ES, R>(row);
+      off[i] = (uint32_t)row * (uint32_t)ld + x * 16;
+      if (KC) k = x * EPC;
+    }
+  }
+  // The next slice into LDS; one past the end of K is zeros.
+  __device__ __forceinline__ void load(char* st) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // (no branches here: with one, the compiler no longer sees which stage a
+    // load in flight goes to, and waits for it before it reads the other)
+    const int e = KC ? max(extent, 0) : max((min(kleft, BKE) - 1) * ld + extent, 0);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, e, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const uint32_t o = KC && k >= kleft ? kPast : off[i];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_any*)(st + (i * NT + wave * 64) * 16), 16, (int)o, 0, 0, 0);
+    }
+    base += step;
+    kleft -= BKE;
+    if (KC) extent -= kSlice;
+  }
+};
+
+// Fragments of 16 rows (columns) from r0 on, as MFMAs take them: lane l holds
+// row l % 16 and, of the slice's half kk, 16 bytes of k (16 bits: k = 32 kk +
+// 8 (l / 16) .. + 7; fp32: 16 kk + 4 (l / 16) .. + 3; e4m3: 64 kk + 16 (l / 16) .. +
+// 15; A and B need only agree).  N of them, 16 rows apart.
+template <int ES, bool KC, int R, int N>
+struct Fragments {
+  static __device__ __forceinline__ void read(const char* st, int r0, int kk, int lane, u32x4* out) {
+    const int li = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = r0 + 16 * i + li;
+      if (KC) {
+        out[i] = *(const u32x4*)(st + r * kSlice + (((4 * kk + g) ^ (li & 7)) << 4));
+      } else {  // fp32
+        const int k = 16 * kk + 4 * g;
+        const char* p = st + k * (R * 4) + (((r >> 2) ^ km_swizzle<4, R>(k)) << 4) + 4 * (r & 3);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) out[i][u] = *(const uint32_t*)(p + u * (R * 4));
+      }
+    }
+  }
+};
+
+// 16 bits, KM, by transposing reads: in each, lane i of a group of 16 gives the
+// address of four columns of k row i / 4 and receives column i of the four
+// rows.  In assembly, two fragments at a time and waited for there: the
+// compiler does not tell which stage such a read goes to, and would wait for
+// the loads in flight to the other one first.
+__device__ __forceinline__ uint32_t lds_offset(const char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+template <int R, int N>
+struct Fragments<2, false, R, N> {
+  static __device__ __forceinline__ void read(const char* st, int r0, int kk, int lane, u32x4* out) {
+    static_assert(N % 2 == 0, "pairs of fragments");
+    const int li = lane & 15, g = lane >> 4;
+    const int k = 8 * g + (li >> 2);
+    const uint32_t p = lds_offset(st) + k * (R * 2) + 8 * (li & 1);
+    const int x = (r0 >> 3) + ((li >> 1) & 1), w = km_swizzle<2, R>(k);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      u32x2 a, b, c, d;
+      asm volatile(
+          "ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
+          "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+          "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
+          "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
+          : "v"(p + (((x + 2 * i) ^ w) << 4)), "v"(p + (((x + 2 * i + 2) ^ w) << 4)), "i"(kk * 32 * R * 2),
+            "i"((kk * 32 + 4) * R * 2)
+          : "memory");
+      out[i] = u32x4{a[0], a[1], b[0], b[1]};
+      out[i + 1] = u32x4{c[0], c[1], d[0], d[1]};
+    }
+  }
+};
+
+template <class E>
+struct Mma;
+template <>
+struct Mma<__bf16> {
+  static __device__ __forceinline__ f32x4 run(u32x4 b, u32x4 a, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<_Float16> {
+  static __device__ __forceinline__ f32x4 run(u32x4 b, u32x4 a, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<float> {
+  static __device__ __forceinline__ f32x4 run(u32x4 b, u32x4 a, f32x4 c) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b[u]), __uint_as_float(a[u]), c, 0, 0, 0);
+    return c;
+  }
+};
+
+// ---- tiles ----
+
+template <int BM_, int BN_, int WM_, int WN_>
+struct TileShape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;  // WM x WN waves
+  static constexpr int NT = 64 * WM * WN, TM = BM / WM, TN = BN / WN;
+  static constexpr int MI = TM / 16, NI = TN / 16;
+  static constexpr int A_BYTES = BM * kSlice, STAGE = A_BYTES + BN * kSlice;
+  static constexpr int ER = 32;      // rows of a wave's block that pass through LDS at a time
+  static constexpr int EP = TN + 4;  // their pitch in floats
+  static_assert(WM * WN / 2 * ER * EP * 4 <= STAGE, "a stage holds half of the waves' rows");
+};
+typedef TileShape<64, 64, 2, 2> TileS;
+typedef TileShape<128, 128, 2, 2> TileM;
+typedef TileShape<256, 256, 2, 4> TileL;
+
+// A wave's products of a slice, in two parts.  16 bits and fp32: a part is half
+// the slice's k.
+template <class E, bool AKC, bool BKC, class Tile>
+struct Parts {
+  static constexpr int ES = ElemSize<E>::value;
+  struct Frag {
+    u32x4 a[Tile::MI], b[Tile::NI];
+  };
+  Frag f[2];
+  template <int P>
+  __device__ __forceinline__ void read(const char* st, int wm, int wn, int lane) {
+    Fragments<ES, BKC, Tile::BN, Tile::NI>::read(st + Tile::A_BYTES, wn, P, lane, f[P].b);
+    Fragments<ES, AKC, Tile::BM, Tile::MI>::read(st, wm, P, lane, f[P].a);
+  }
+  template <int P>
+  __device__ __forceinline__ void mma(f32x4 (&acc)[Tile::MI][Tile::NI]) {
+#pragma unroll
+    for (int i = 0; i < Tile::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < Tile::NI; ++j) acc[i][j] = Mma<E>::run(f[P].b[j], f[P].a[i], acc[i][j]);
+  }
+};
+
+// e4m3: a part is half of the wave's rows.
+template <bool WIDE, class Tile>
+struct Fp8Parts {
+  static constexpr int H = Tile::MI / 2;
+  u32x4 b[2][Tile::NI], a[2][H];
+  template <int P>
+  __device__ __forceinline__ void read(const char* st, int wm, int wn, int lane) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      if (P == 0) Fragments<1, true, Tile::BN, Tile::NI>::read(st + Tile::A_BYTES, wn, kk, lane, b[kk]);
+      Fragments<1, true, Tile::BM, H>::read(st, wm + 16 * H * P, kk, lane, a[kk]);
+    }
+  }
+  template <int P>
+  __device__ __forceinline__ void mma(f32x4 (&acc)[Tile::MI][Tile::NI]) {
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < H; ++i)
+#pragma unroll
+        for (int j = 0; j < Tile::NI; ++j)
+          // operand formats 0: e4m3; block scales 2^0
+          acc[H * P + i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+              join(b[0][j], b[1][j]), join(a[0][i], a[1][i]), acc[H * P + i][j], 0, 0, 0, 127, 0, 127);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f16x8 w[Tile::NI];
+#pragma unroll
+        for (int j = 0; j < Tile::NI; ++j) w[j] = eight(b[q / 2][j], q);
+#pragma unroll
+        for (int i = 0; i < H; ++i) {
+          const f16x8 x = eight(a[q / 2][i], q);
+#pragma unroll
+          for (int j = 0; j < Tile::NI; ++j)
+            acc[H * P + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[j], x, acc[H * P + i][j], 0, 0, 0);
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ i32x8 join(u32x4 lo, u32x4 hi) {
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  }
+  // bytes 8 (q % 2) .. + 7 of a fragment
+  static __device__ __forceinline__ f16x8 eight(u32x4 v, int q) {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    f16x8 r;
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const uint32_t w = v[q % 2 * 2 + d];
+      const f16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
+      const f16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true);
+      r[4 * d] = lo[0], r[4 * d + 1] = lo[1], r[4 * d + 2] = hi[0], r[4 * d + 3] = hi[1];
+    }
+    return r;
+  }
+};
+template <bool AKC, bool BKC, class Tile>
+struct Parts<Fp8, AKC, BKC, Tile> : Fp8Parts<false, Tile> {};
+template <bool AKC, bool BKC, class Tile>
+struct Parts<Fp8Wide, AKC, BKC, Tile> : Fp8Parts<true, Tile> {};
+
+// The tile of a workgroup.  Workgroup b runs on XCD b % 8: each XCD takes a
+// contiguous share of the tiles, and tiles follow each other down `GM` rows
+// and then along, so that those in flight on an XCD share rows and columns in
+// its L2.
+__device__ __forceinline__ void tile_of(const GemmArgs& P, int GM, int& c, int& split, int& tm, int& tn) {
+  const int total = gridDim.x, q = total >> 3, r = total & 7, x = blockIdx.x & 7;
+  int t = x * q + min(x, r) + (blockIdx.x >> 3);
+  const int per = P.tiles_m * P.tiles_n;
+  const int cs = t / per;
+  t -= cs * per;
+  c = cs / P.splits;
+  split = cs - c * P.splits;
+  const int band = GM * P.tiles_n, first = t / band * GM, rows = min(P.tiles_m - first, GM);
+  t %= band;
+  tm = first + t % rows;
+  tn = t / rows;
+}
+
+template <class E, class T, bool AKC, bool BKC, class Tile>
+__global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) {
+  constexpr int ES = ElemSize<E>::value, BKE = kSlice / ES;
+  // two arrays, not one: a load into one stage is then seen not to touch the
+  // other, and reads of that one do not wait for it
+  __shared__ __attribute__((aligned(1024))) char stage0[Tile::STAGE], stage1[Tile::STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / Tile::WN * Tile::TM, wn = wave % Tile::WN * Tile::TN;
+  int c, split, tm, tn;
+  tile_of(P, 4, c, split, tm, tn);
+  const int m0 = tm * Tile::BM, n0 = tn * Tile::BN;
+  const int k0 = split * P.per_split * BKE, kend = min(P.K, k0 + P.per_split * BKE);
+
+  Operand<ES, AKC, Tile::BM, Tile::NT> A;
+  Operand<ES, BKC, Tile::BN, Tile::NT> B;
+  A.init(P.A + c * P.a_cell, P.a_ld, m0, P.M, kend, k0);
+  B.init(P.B + c * P.b_cell, P.b_ld, n0, P.N, kend, k0);
+  auto load = [&](char* st) {
+    A.load(st);
+    B.load(st + Tile::A_BYTES);
+  };
+  f32x4 acc[Tile::MI][Tile::NI] = {};
+  Parts<E, AKC, BKC, Tile> F;
+  load(stage0);
+  // One slice, in `cur`.
+  auto step = [&](char* cur, char* next) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's loads of the slice have landed
+    __syncthreads();                     // and every wave has read the one before
+    load(next);
+    F.template read<0>(cur, wm, wn, lane);
+    F.template mma<0>(acc);
+    F.template read<1>(cur, wm, wn, lane);
+    F.template mma<1>(acc);
+  };
+  for (int k = k0; k < kend; k += 2 * BKE) {  // a slice past the end is zeros
+    step(stage0, stage1);
+    step(stage1, stage0);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+
+  // a lane's columns are the same in every row it finishes
+  constexpr int LPR = Tile::TN / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
+  const int li = lane & 15, g = lane >> 4;
+  const int n = n0 + wn + 8 * (lane % LPR), left = P.N - n;
+  constexpr int HALF = Tile::WM * Tile::WN / 2;
+  float* mine = (float*)(wave < HALF ? stage0 : stage1) + (wave % HALF) * (Tile::ER * Tile::EP);
+  const bool sums = P.splits > 1;
+  const f32x8 bias = sums ? f32x8{} : column8(P.f.bias, P.f.bias_cell, c, n, left);
+  const f32x8 ws = sums ? f32x8{} : column8(P.f.ws, P.f.ws_cell, c, n, left);
+  float* part = P.part + ((int64_t)split * P.cells + c) * P.M * P.part_ld;
+#pragma unroll
+  for (int h = 0; h < Tile::TM / Tile::ER; ++h) {
+    if (h) __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < Tile::ER / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < Tile::NI; ++j)
+        *(f32x4*)(mine + (16 * i + li) * Tile::EP + 16 * j + 4 * g) = acc[h * (Tile::ER / 16) + i][j];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    for (int p = 0; p < Tile::ER / RPP; ++p) {
+      const int row = p * RPP + lane / LPR, m = m0 + wm + h * Tile::ER + row;
+      if (m >= P.M || left <= 0) continue;
+      const f32x4 lo = *(const f32x4*)(mine + row * Tile::EP + 8 * (lane % LPR));
+      const f32x4 hi = *(const f32x4*)(mine + row * Tile::EP + 8 * (lane % LPR) + 4);
+      const f32x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      if (sums) store8(part + (int64_t)m * P.part_ld + n, 8, v);
+      else finish8<T>(P.f, c, m, n, left, v, bias, ws);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  }
+}
+
+// The splits' sums, in order, and the finish.  A thread takes 8 columns of a row.
+template <class T>
+__global__ __launch_bounds__(256) void join_splits_kernel(const GemmArgs P) {
+  const int per_row = P.part_ld / 8;
+  const int64_t rows = (int64_t)P.cells * P.M;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= rows * per_row) return;
+  const int64_t row = at / per_row;
+  const int n = 8 * (int)(at - row * per_row), c = (int)(row / P.M), m = (int)(row - (int64_t)c * P.M), left = P.N - n;
+  const float* p = P.part + row * P.part_ld + n;
+  f32x8 v = load8(p, 8);
+  for (int s = 1; s < P.splits; ++s) {
+    p += rows * P.part_ld;
+    const f32x8 w = load8(p, 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  }
+  finish8<T>(P.f, c, m, n, left, v, column8(P.f.bias, P.f.bias_cell, c, n, left),
+             column8(P.f.ws, P.f.ws_cell, c, n, left));
+}
+
+// ---- the host's checks, operands and workspaces ----
+
+inline bool valid_block_act(int a, float slope) {
+  return a >= LIPZ_ACT_LINEAR && a <= LIPZ_ACT_SILU && (a != LIPZ_ACT_LRELU || (slope > 0.f && slope < __builtin_inff()));
+}
+
+inline lipz_status check_sizes(int cells, int rows, int fan_in, int fan_out) {
+  if (cells < 1 || rows < 0 || fan_in < 1 || fan_out < 1) return LIPZ_E_INVAL;
+  if (cells > kMaxCells || rows > kMaxRows || fan_in > kMaxWide || fan_out > kMaxWide) return LIPZ_E_UNSUPPORTED;
+  return LIPZ_OK;
+}
+
+inline void set_operands(GemmArgs& P, const lipz_mat& A, const lipz_mat& B, int es, int M, int N, int K, int cells) {
+  P.A = (const char*)A.p, P.a_ld = A.ld * es, P.a_cell = A.cell * es;
+  P.B = (const char*)B.p, P.b_ld = B.ld * es, P.b_cell = B.cell * es;
+  P.M = M, P.N = N, P.K = K, P.cells = cells;
+}
+
+// A workspace's parts, each from a multiple of 256 bytes on.
+struct Bump {
+  size_t at = 0;
+  size_t take(size_t n) {
+    const size_t p = at;
+    at += (n + 255) / 256 * 256;
+    return p;
+  }
+};
+
+// Whether an operand [rows][cols] can go straight into LDS; kc: k along its rows.
+inline bool loads_as_is(const lipz_mat& m, int64_t cols, int es, bool kc) {
+  return ((uintptr_t)m.p & 3) == 0 && (m.ld * es) % 4 == 0 && (m.cell * es) % 4 == 0 && (cols * es) % (kc ? 16 : 4) == 0;
+}
+inline int64_t packed_ld(int64_t cols, int es) { return (cols * es + 63) / 64 * 64 / es; }
+inline size_t packed_bytes(int64_t rows, int64_t cols, int es, int cells) {
+  return (size_t)cells * rows * packed_ld(cols, es) * es;
+}
+
+// Copies [cells][rows][cols] into rows of whole 64-byte blocks (dst, zeros past
+// cols).  W: an unsigned integer of the elements' size.
+template <class W>
+__global__ __launch_bounds__(256) void pack_kernel(const W* src, int64_t ld, int64_t cell, W* dst, int64_t dst_ld, int rows,
+                                                   int cols) {
+  constexpr int EPC = 16 / (int)sizeof(W);
+  struct __attribute__((packed, aligned(sizeof(W)))) Chunk {
+    u32x4 v;
+  };
+  const int per = (int)dst_ld / EPC;
+  const int64_t n = (int64_t)rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / per;
+    const int col = (int)(i - row * per) * EPC, left = cols - col;
+    const LIPZ_GLOBAL W* p = as_global(src) + blockIdx.y * cell + row * ld + col;
+    u32x4 w = {};
+    if (left >= EPC) {
+      w = reinterpret_cast<const LIPZ_GLOBAL Chunk*>(p)->v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < EPC - 1; ++e)
+        if (e < left) w[e * (int)sizeof(W) / 4] |= (uint32_t)p[e] << (8 * (e * (int)sizeof(W) % 4));
+    }
+    *reinterpret_cast<LIPZ_GLOBAL u32x4*>(as_global(dst) + ((int64_t)blockIdx.y * rows + row) * dst_ld + col) = w;
+  }
+}
+template <class W>
+inline lipz_mat launch_pack(const lipz_mat& m, void* dst, int rows, int cols, int cells, hipStream_t s) {
+  const int64_t ld = packed_ld(cols, sizeof(W)), chunks = (int64_t)rows * ld * sizeof(W) / 16;
+  const int64_t blocks = (chunks + 255) / 256, most = 4096 / cells + 1;
+  pack_kernel<W><<<dim3((unsigned)(blocks < most ? blocks : most), cells), 256, 0, s>>>((const W*)m.p, m.ld, m.cell, (W*)dst, ld,
+                                                                                    rows, cols);
+  return lipz_mat{dst, ld, rows * ld};
+}
+
+// ---- the host's choices ----
+
+enum { TILE_S = 0, TILE_M = 1, TILE_L = 2 };
+struct Plan {
+  int tile, splits, per_split;
+  size_t part_bytes;
+};
+
+inline int tiles_of(int n, int b) { return (n + b - 1) / b; }
+
+inline Plan plan_gemm(int es, int M, int N, int K, int cells) {
+  Plan p{TILE_S, 1, 0, 0};
+  const int64_t l = (int64_t)tiles_of(M, 256) * tiles_of(N, 256) * cells, m = (int64_t)tiles_of(M, 128) * tiles_of(N, 128) * cells;
+  if (es < 4 && l >= 192) p.tile = TILE_L;
+  else if (m >= 192) p.tile = TILE_M;
+  const int b = p.tile == TILE_L ? 256 : p.tile == TILE_M ? 128 : 64;
+  const int64_t tiles = (int64_t)tiles_of(M, b) * tiles_of(N, b) * cells;
+  const int slices = tiles_of(K * es, kSlice);
+  int splits = 1;
+  if (p.tile == TILE_S && tiles < 256) {
+    splits = (int)(512 / tiles);
+    if (splits > slices / 4) splits = slices / 4;
+    if (splits < 1) splits = 1;
+  }
+  p.per_split = tiles_of(slices, splits);
+  p.splits = tiles_of(slices, p.per_split);
+  if (p.splits > 1) p.part_bytes = (size_t)p.splits * cells * M * (size_t)((N + 7) / 8 * 8) * 4;
+  return p;
+}
+
+template <class E, class T, bool AKC, bool BKC>
+inline void launch_gemm(GemmArgs& P, const Plan& plan, hipStream_t s) {
+  const int b = plan.tile == TILE_L ? 256 : plan.tile == TILE_M ? 128 : 64;
+  P.tiles_m = tiles_of(P.M, b);
+  P.tiles_n = tiles_of(P.N, b);
+  P.splits = plan.splits;
+  P.per_split = plan.per_split;
+  P.part_ld = (P.N + 7) / 8 * 8;
+  const dim3 grid((unsigned)(P.tiles_m * P.tiles_n * P.cells * P.splits));
+#define LIPZ_TILE(ID, TILE) \
+  if (plan.tile == ID) block_gemm_kernel<E, T, AKC, BKC, TILE><<<grid, TILE::NT, 0, s>>>(P);
+  LIPZ_TILE(TILE_S, TileS)
+  LIPZ_TILE(TILE_M, TileM)
+  if constexpr (ElemSize<E>::value < 4) {
+    LIPZ_TILE(TILE_L, TileL)
+  }
+#undef LIPZ_TILE
+  if (P.splits > 1) {
+    const int64_t threads = (int64_t)P.cells * P.M * (P.part_ld / 8);
+    join_splits_kernel<T><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, s>>>(P);
+  }
+}
+
+}  // namespace lipz

@@ -117,8 +117,17 @@ lipz_rms_norm_args = _args("lipz_rms_norm_args", "dtype y_dtype cells rows cols"
                            "f:eps m:x m:residual m:h m:y p:gamma l:gamma_cell p:rstd p:y_scale")
 lipz_rms_norm_backward_args = _args("lipz_rms_norm_backward_args", "dtype cells rows cols",
                                     "m:h m:dy m:dh m:dx p:gamma l:gamma_cell p:rstd p:dgamma l:dgamma_cell")
-#LINEAR_ARGS
-_BLOCK = {c.__name__[:-5]: c for c in (lipz_rms_norm_args, lipz_rms_norm_backward_args)}
+lipz_linear_args = _args("lipz_linear_args", "dtype cells rows fan_in fan_out act",
+                         "f:slope m:x m:w m:residual m:pre m:y p:bias l:bias_cell")
+lipz_linear_backward_args = _args("lipz_linear_backward_args", "dtype cells rows fan_in fan_out act",
+                                  "f:slope m:x m:w m:pre m:dy m:dx m:dw p:db l:db_cell")
+lipz_quantize_weights_args = _args("lipz_quantize_weights_args", "dtype cells fan_in fan_out",
+                                   "m:w m:q p:scale l:scale_cell")
+lipz_linear_fp8_args = _args("lipz_linear_fp8_args", "y_dtype cells rows fan_in fan_out act",
+                             "f:slope m:x m:w m:residual m:y p:x_scale l:x_scale_cell p:w_scale l:w_scale_cell "
+                             "p:bias l:bias_cell")
+_BLOCK = {c.__name__[:-5]: c for c in (lipz_rms_norm_args, lipz_rms_norm_backward_args, lipz_linear_args,
+                                       lipz_linear_backward_args, lipz_quantize_weights_args, lipz_linear_fp8_args)}
 
 _SIGS = {
     "lipz_workspace_bytes": (_sz, [ctypes.POINTER(lipz_config), _i64]),
@@ -336,6 +345,42 @@ def lipz_rms_norm_backward_workspace_bytes(args):
 def lipz_rms_norm_backward(args, d_workspace, workspace_bytes, stream):
     return _check(load_library().lipz_rms_norm_backward(ctypes.byref(args), d_workspace, workspace_bytes, stream),
                   "lipz_rms_norm_backward")
+
+
+def lipz_linear_workspace_bytes(args):
+    return load_library().lipz_linear_workspace_bytes(ctypes.byref(args))
+
+
+def lipz_linear(args, d_workspace, workspace_bytes, stream):
+    return _check(load_library().lipz_linear(ctypes.byref(args), d_workspace, workspace_bytes, stream),
+                  "lipz_linear")
+
+
+def lipz_linear_backward_workspace_bytes(args):
+    return load_library().lipz_linear_backward_workspace_bytes(ctypes.byref(args))
+
+
+def lipz_linear_backward(args, d_workspace, workspace_bytes, stream):
+    return _check(load_library().lipz_linear_backward(ctypes.byref(args), d_workspace, workspace_bytes, stream),
+                  "lipz_linear_backward")
+
+
+def lipz_quantize_weights_workspace_bytes(args):
+    return load_library().lipz_quantize_weights_workspace_bytes(ctypes.byref(args))
+
+
+def lipz_quantize_weights(args, d_workspace, workspace_bytes, stream):
+    return _check(load_library().lipz_quantize_weights(ctypes.byref(args), d_workspace, workspace_bytes, stream),
+                  "lipz_quantize_weights")
+
+
+def lipz_linear_fp8_workspace_bytes(args):
+    return load_library().lipz_linear_fp8_workspace_bytes(ctypes.byref(args))
+
+
+def lipz_linear_fp8(args, d_workspace, workspace_bytes, stream):
+    return _check(load_library().lipz_linear_fp8(ctypes.byref(args), d_workspace, workspace_bytes, stream),
+                  "lipz_linear_fp8")
 
 
 def lipz_test_gemm(stream, d_desc, M, N, K, d_A, lda, a_trans, ones_row, d_B, ldb, b_trans, d_C, ldc,

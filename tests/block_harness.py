@@ -21,7 +21,7 @@ def mat(t):
 
 def padded(g, cells, rows, cols, dtype, pad, scale=1.0, off=0):
     """[cells][rows][cols] inside a larger allocation whose other elements are NaN."""
-    big = torch.full((cells * (rows * (cols + pad) + 3) + off + 8,), float("nan"), dtype=dtype, device="cuda")
+    big = torch.full((cells * (rows * (cols + pad) + 3) + off + 8,), float("nan"), device="cuda").to(dtype)
     t = big[off:off + cells * (rows * (cols + pad) + 3)].view(cells, -1)[:, :rows * (cols + pad)]
     t = t.as_strided((cells, rows, cols), (t.stride(0), cols + pad, 1), big.storage_offset() + off)
     t.copy_((torch.randn(cells, rows, cols, generator=g, device="cuda") * scale).to(dtype))

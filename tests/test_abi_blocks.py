@@ -30,6 +30,32 @@ def norm_bwd(**kw):
 
 
 NONE = L.lipz_mat()
+
+
+def linear(**kw):
+    d = dict(dtype=L.LIPZ_BF16, cells=2, rows=4, fan_in=24, fan_out=40, act=L.LIPZ_ACT_LRELU, slope=0.2, x=mat(24),
+             w=mat(40, 24), residual=mat(40), pre=mat(40), y=mat(40), bias=P, bias_cell=40)
+    return L.lipz_linear_args(**dict(d, **kw))
+
+
+def linear_bwd(**kw):
+    d = dict(dtype=L.LIPZ_BF16, cells=2, rows=4, fan_in=24, fan_out=40, act=L.LIPZ_ACT_SILU, slope=0.2, x=mat(24),
+             w=mat(40, 24), pre=mat(40), dy=mat(40), dx=mat(24), dw=mat(40, 24), db=P, db_cell=40)
+    return L.lipz_linear_backward_args(**dict(d, **kw))
+
+
+def quant(**kw):
+    d = dict(dtype=L.LIPZ_BF16, cells=2, fan_in=24, fan_out=40, w=mat(40, 24), q=mat(24, 40), scale=P, scale_cell=40)
+    return L.lipz_quantize_weights_args(**dict(d, **kw))
+
+
+def linear_fp8(**kw):
+    d = dict(y_dtype=L.LIPZ_BF16, cells=2, rows=4, fan_in=24, fan_out=40, act=L.LIPZ_ACT_GELU, slope=0.2, x=mat(24),
+             w=mat(24, 40), residual=mat(40), y=mat(40), x_scale=P, x_scale_cell=4, w_scale=P, w_scale_cell=40, bias=P,
+             bias_cell=40)
+    return L.lipz_linear_fp8_args(**dict(d, **kw))
+
+
 BAD = {
     "lipz_rms_norm": (norm, [
         dict(dtype=3), dict(dtype=-1), dict(y_dtype=L.LIPZ_F32), dict(cells=0), dict(rows=-1), dict(cols=0), dict(eps=0.0),
@@ -43,6 +69,27 @@ BAD = {
         dict(gamma=None), dict(rstd=None), dict(rstd=P + 1), dict(dy=mat(24, ld=8)), dict(dx=mat(24, cell=24)),
         dict(dgamma_cell=23), dict(dgamma=P + 1)], [
         dict(dh=mat(24, ld=(1 << 20) + 8)), dict(cells=65536)]),
+    "lipz_linear": (linear, [
+        dict(dtype=3), dict(cells=0), dict(rows=-1), dict(fan_in=0), dict(fan_out=0), dict(act=6), dict(act=-1),
+        dict(slope=0.0), dict(slope=float("inf")), dict(x=NONE), dict(w=NONE), dict(y=NONE), dict(x=mat(23)),
+        dict(w=mat(39, 24)), dict(y=mat(40, cell=40)), dict(pre=mat(40, p=P + 1)), dict(residual=mat(40, cell=-1)),
+        dict(bias=P + 2), dict(bias_cell=-1)], [
+        dict(cells=65536), dict(rows=(1 << 21) + 1), dict(fan_in=(1 << 20) + 1), dict(x=mat(24, ld=(1 << 20) + 2)),
+        dict(rows=1 << 21, fan_out=1 << 20, w=mat(1 << 20, 24), residual=NONE, pre=NONE, y=mat(1 << 20, 1 << 21))]),
+    "lipz_linear_backward": (linear_bwd, [
+        dict(dtype=3), dict(cells=0), dict(rows=-1), dict(fan_in=0), dict(fan_out=0), dict(act=7), dict(pre=NONE),
+        dict(dy=NONE), dict(x=NONE), dict(w=NONE), dict(dx=NONE, dw=NONE, db=None), dict(dx=mat(24, cell=24)),
+        dict(dw=mat(40, 24, cell=0)), dict(db_cell=39), dict(act=L.LIPZ_ACT_LRELU, slope=-1.0), dict(dy=mat(39))], [
+        dict(cells=65536), dict(rows=(1 << 21) + 1), dict(w=mat(40, 24, ld=(1 << 20) + 2))]),
+    "lipz_quantize_weights": (quant, [
+        dict(dtype=3), dict(cells=0), dict(fan_in=0), dict(fan_out=0), dict(w=NONE), dict(q=NONE), dict(scale=None),
+        dict(q=mat(23, 40)), dict(q=mat(24, 40, cell=24)), dict(scale_cell=39), dict(scale=P + 1)], [
+        dict(cells=65536), dict(fan_out=(1 << 20) + 1)]),
+    "lipz_linear_fp8": (linear_fp8, [
+        dict(y_dtype=3), dict(cells=0), dict(rows=-1), dict(fan_in=0), dict(fan_out=0), dict(act=6), dict(x=NONE),
+        dict(w=NONE), dict(y=NONE), dict(x_scale=None), dict(w_scale=None), dict(w=mat(23, 40)), dict(y=mat(40, cell=39)),
+        dict(x_scale=P + 1), dict(x_scale_cell=-4)], [
+        dict(cells=65536), dict(rows=(1 << 21) + 1)]),
 }
 
 
@@ -71,14 +118,19 @@ def test_refusals(name):
     assert getattr(lib, name + "_workspace_bytes")(None) == 0
 
 
-@pytest.mark.parametrize("name", sorted(BAD))
-def test_cells_inside_rows_and_shared_inputs_are_taken(name):
-    make, need = BAD[name][0], getattr(L, name + "_workspace_bytes")
-    side = lambda: L.lipz_mat(P, 48, 24)  # noqa: E731  two cells side by side in a row
-    kw = dict(y=side(), x=side()) if name == "lipz_rms_norm" else dict(dx=side(), dy=side())
-    assert need(make(**kw)) > 0
-    kw = dict(x=mat(24, cell=0), gamma_cell=0) if name == "lipz_rms_norm" else dict(h=mat(24, cell=0), gamma_cell=0)
-    assert need(make(**kw)) > 0
+@pytest.mark.parametrize("make,name,kw", [
+    (norm, "lipz_rms_norm", dict(y=L.lipz_mat(P, 48, 24), x=L.lipz_mat(P, 48, 24))),
+    (norm, "lipz_rms_norm", dict(x=mat(24, cell=0), gamma_cell=0)),
+    (norm_bwd, "lipz_rms_norm_backward", dict(dx=L.lipz_mat(P, 48, 24), dy=L.lipz_mat(P, 48, 24))),
+    (norm_bwd, "lipz_rms_norm_backward", dict(h=mat(24, cell=0), gamma_cell=0)),
+    (linear, "lipz_linear", dict(y=L.lipz_mat(P, 80, 40), x=mat(24, cell=0), w=mat(40, 24, cell=0), bias_cell=0)),
+    (linear_bwd, "lipz_linear_backward", dict(act=L.LIPZ_ACT_LINEAR, pre=NONE)),
+    (linear_bwd, "lipz_linear_backward", dict(dx=NONE, w=NONE)),
+    (linear_bwd, "lipz_linear_backward", dict(dw=NONE, x=NONE, db=None)),
+    (linear_fp8, "lipz_linear_fp8", dict(x=mat(24, cell=0), w_scale_cell=0, bias=None, residual=NONE))])
+def test_cells_inside_rows_shared_inputs_and_left_out_ones_are_taken(make, name, kw):
+    """Cells side by side in a row, inputs shared by the cells, optional matrices left out."""
+    assert getattr(L, name + "_workspace_bytes")(make(**kw)) > 0
 
 
 @pytest.mark.parametrize("name", ["lipz_mat"] + [n + "_args" for n in sorted(BAD)])
