@@ -421,7 +421,9 @@ typedef struct {
  *   y = h * rstd * gamma
  * h is rounded to dtype for its store only: rstd and y come from the fp32 sum.
  * y_dtype: dtype, or LIPZ_FP8 with a scale per row,
- *   y_scale[i] = max(max_j |h rstd gamma| / 448, 2^-126),  y = e4m3(h rstd gamma / y_scale);
+ *   y_scale[i] = max(max_j |h rstd gamma| / 448, 2^-126),  y = e4m3(h rstd gamma / y_scale)
+ * (the division by 448 is a product with its fp32 reciprocal, the other a
+ * division);
  * a row that holds a NaN or an infinity then has the scale NaN and only NaN in
  * y.  residual, h and rstd may be NULL; h may be x or residual itself (same p,
  * ld and cell).  rows >= 0, 1 <= cols <= 2^20, eps > 0. */
@@ -494,8 +496,8 @@ lipz_status lipz_linear_backward(const lipz_linear_backward_args* a, void* d_wor
 
 /* Weights for lipz_linear_fp8: column j of w [fan_in][fan_out] becomes row j
  * of q [fan_out][fan_in] (LIPZ_FP8) with
- *   scale[j] = max(max_k |w[k][j]| / 448, 2^-126),  q[j][k] = e4m3(w[k][j] / scale[j]);
- * a column that holds a NaN or an infinity has the scale NaN and only NaN. */
+ *   scale[j] = max(max_k |w[k][j]| / 448, 2^-126),  q[j][k] = e4m3(w[k][j] / scale[j])
+ * with the divisions of lipz_rms_norm; a column that holds a NaN or an infinity has the scale NaN and only NaN. */
 typedef struct {
   int32_t abi_version, dtype, cells, fan_in, fan_out;
   lipz_mat w, q;

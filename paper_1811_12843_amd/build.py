@@ -7,6 +7,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -37,20 +39,32 @@ def sources():
 
 def build(verbose=False, out=None, defines=()):
     """Compile every HIP source into paper_1811_12843_amd/liblipz.so (or `out`),
-    with optional -D definitions."""
+    with optional -D definitions.  The sources are compiled side by side, each
+    into an object file of its own, and linked."""
     lib = out or LIB
     tmp = lib + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, *["-D" + d for d in defines], "-I", os.path.join(ROOT, "include"),
-           "-I", os.path.join(PKG, "csrc"), *sources(), "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    msgs = "\n".join(l for l in (r.stdout + r.stderr).splitlines()
-                     if "packed-fp32-ops" not in l and "is not a recognized feature" not in l)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + msgs)
-    if verbose and msgs.strip():
-        print(msgs)
+    flags = [*HIPCC_FLAGS, *["-D" + d for d in defines], "-I", os.path.join(ROOT, "include"),
+             "-I", os.path.join(PKG, "csrc")]
+    msgs = []
+
+    def run(cmd):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        text = "\n".join(l for l in (r.stdout + r.stderr).splitlines()
+                         if "packed-fp32-ops" not in l and "is not a recognized feature" not in l)
+        if r.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + text)
+        msgs.append(text)
+
+    with tempfile.TemporaryDirectory() as d:
+        jobs = [(src, os.path.join(d, os.path.basename(src) + ".o")) for src in sources()]
+        compiles = [[hipcc(), *[f for f in flags if f != "-shared"], "-c", src, "-o", obj] for src, obj in jobs]
+        if verbose:
+            print(*(" ".join(c) for c in compiles), sep="\n", flush=True)
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(run, compiles))
+        run([hipcc(), *HIPCC_FLAGS, *[obj for _, obj in jobs], "-o", tmp])
+    if verbose and any(m.strip() for m in msgs):
+        print("\n".join(m for m in msgs if m.strip()))
     os.replace(tmp, lib)
     return lib
 

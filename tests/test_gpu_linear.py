@@ -247,7 +247,7 @@ def test_quantize_weights(size, dtype):
                                          scale=scale.data_ptr(), scale_cell=N + 1)
         call("lipz_quantize_weights", a)
         want = torch.clamp_min(w.double().abs().amax(1) / 448, 2.0 ** -126)
-        close(scale[:, :N], want, "f32", 0.0, "scale")
+        close(scale[:, :N], want, "f32", 2.0 ** -24 * want, "scale")  # 1 / 448 is rounded, then the product
         # the quotient by the fp32 scale, once rounded in fp32
         close(q, w.double().mT / scale[:, :N].double()[:, :, None], "fp8", 448 * 2.0 ** -24, "q")
         assert ok() and bool((scale[:, N] == 7).all())
