@@ -48,6 +48,31 @@ __device__ __forceinline__ f32x8 load8(const T* p, int n) {
     if (e < n) r[e] = (float)as_global(p)[e];
   return r;
 }
+// Hides from the compiler what a raw eight holds, so that it converts it again
+// instead of keeping the fp32 values in registers.
+template <class V>
+__device__ __forceinline__ void forget(V& v) {
+  if constexpr (sizeof(V) == 16) {
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+    asm volatile("" : "+v"(w));
+    v = __builtin_bit_cast(V, w);
+  }
+}
+
+// Elements as load8 takes them, not yet converted.
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type load8_raw(const T* p, int n) {
+  if (n >= 8) return reinterpret_cast<const LIPZ_GLOBAL Eight<T>*>((const LIPZ_GLOBAL T*)p)->v;
+  typename Vec8<T>::type r = {};
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) r[e] = as_global(p)[e];
+  return r;
+}
+template <class T>
+__device__ __forceinline__ f32x8 widen(typename Vec8<T>::type v) {
+  return __builtin_convertvector(v, f32x8);
+}
 template <class T>
 __device__ __forceinline__ void store8(T* p, int n, f32x8 v) {
   const typename Vec8<T>::type w = __builtin_convertvector(v, typename Vec8<T>::type);

@@ -7,11 +7,8 @@
 // row: A stored [K][M], B [K][N]).
 //
 // A workgroup owns a BM x BN tile and walks K in slices of 128 bytes per row
-// (32 k of fp32, 64 of 16 bits, 128 of e4m3) through two LDS stages.  A slice is
-// multiplied in two parts: the second part's fragments are read before the
-// first one's MFMAs, the next slice's first ones before the second's, and the
-// slice after the next is asked for as soon as every wave holds the present
-// one in registers; one barrier per slice.
+// (32 k of fp32, 64 of 16 bits, 128 of e4m3) through NS LDS stages, NS - 1 slices
+// in flight ahead of the one that is multiplied; one barrier per slice.
 //
 // LDS.  KC: a row of 128 bytes is eight 16-byte chunks, chunk c at place
 // c ^ (row % 8), so that the 16 rows that a fragment read touches lie on all
@@ -86,8 +83,12 @@ constexpr uint32_t kPast = 0x80000000u;
 
 // ---- finishing: 8 columns of a row from column n on, `left` of them inside ----
 template <class T>
+__device__ __forceinline__ typename Vec8<T>::type residual8(const Finish& f, int c, int m, int n, int left) {
+  return f.r ? load8_raw((const T*)f.r + c * f.r_cell + m * f.r_ld + n, left) : typename Vec8<T>::type{};
+}
+template <class T>
 __device__ __forceinline__ void finish8(const Finish& f, int c, int m, int n, int left, f32x8 v, const f32x8& bias,
-                                        const f32x8& ws) {
+                                        const f32x8& ws, typename Vec8<T>::type residual) {
   constexpr bool FAST = sizeof(T) < 4;
   if (f.xs) {
     const float xs = as_global(f.xs)[c * f.xs_cell + m];
@@ -102,7 +103,7 @@ __device__ __forceinline__ void finish8(const Finish& f, int c, int m, int n, in
     for (int e = 0; e < 8; ++e) v[e] = act_of<FAST>(f.act, v[e], f.slope);
   }
   if (f.r) {
-    const f32x8 r = load8((const T*)f.r + c * f.r_cell + m * f.r_ld + n, left);
+    const f32x8 r = widen<T>(residual);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += r[e];
   }
@@ -260,19 +261,38 @@ struct Mma<float> {
 
 // ---- tiles ----
 
-template <int BM_, int BN_, int WM_, int WN_>
+#ifndef LIPZ_NS_S
+#define LIPZ_NS_S 4
+#endif
+#ifndef LIPZ_NS_M
+#define LIPZ_NS_M 4
+#endif
+template <int BM_, int BN_, int WM_, int WN_, int NS_>
 struct TileShape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;  // WM x WN waves
+  static constexpr int NS = NS_;                                // LDS stages
   static constexpr int NT = 64 * WM * WN, TM = BM / WM, TN = BN / WN;
   static constexpr int MI = TM / 16, NI = TN / 16;
   static constexpr int A_BYTES = BM * kSlice, STAGE = A_BYTES + BN * kSlice;
-  static constexpr int ER = 32;      // rows of a wave's block that pass through LDS at a time
-  static constexpr int EP = TN + 4;  // their pitch in floats
+  static constexpr int LOADS = STAGE / 16 / NT;  // of a slice, per wave
+  static constexpr int ER = 32;                  // rows of a wave's block that pass through LDS at a time
+  static constexpr int EP = TN + 4;              // their pitch in floats
   static_assert(WM * WN / 2 * ER * EP * 4 <= STAGE, "a stage holds half of the waves' rows");
 };
-typedef TileShape<64, 64, 2, 2> TileS;
-typedef TileShape<128, 128, 2, 2> TileM;
-typedef TileShape<256, 256, 2, 4> TileL;
+typedef TileShape<64, 64, 2, 2, LIPZ_NS_S> TileS;
+typedef TileShape<128, 128, 2, 2, LIPZ_NS_M> TileM;
+typedef TileShape<256, 256, 2, 4, 2> TileL;
+
+// Waits until all but this wave's last n vector loads have landed and its LDS
+// accesses are done, then for the other waves.  No more than that: the
+// compiler's barrier would wait for every load.
+template <int n>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4 << 14) | 0x0070);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // A wave's products of a slice, in two parts.  16 bits and fp32: a part is half
 // the slice's k.
@@ -379,9 +399,11 @@ __device__ __forceinline__ void tile_of(const GemmArgs& P, int GM, int& c, int& 
 template <class E, class T, bool AKC, bool BKC, class Tile>
 __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) {
   constexpr int ES = ElemSize<E>::value, BKE = kSlice / ES;
-  // two arrays, not one: a load into one stage is then seen not to touch the
-  // other, and reads of that one do not wait for it
+  // separate arrays: a load into one stage is then seen not to touch the
+  // others, and reads of those do not wait for it
+  constexpr int NS = Tile::NS;
   __shared__ __attribute__((aligned(1024))) char stage0[Tile::STAGE], stage1[Tile::STAGE];
+  __shared__ __attribute__((aligned(1024))) char stage2[NS > 2 ? Tile::STAGE : 16], stage3[NS > 3 ? Tile::STAGE : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / Tile::WN * Tile::TM, wn = wave % Tile::WN * Tile::TN;
   int c, split, tm, tn;
@@ -400,22 +422,30 @@ __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) 
   f32x4 acc[Tile::MI][Tile::NI] = {};
   Parts<E, AKC, BKC, Tile> F;
   load(stage0);
-  // One slice, in `cur`.
-  auto step = [&](char* cur, char* next) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's loads of the slice have landed
-    __syncthreads();                     // and every wave has read the one before
-    load(next);
+  if constexpr (NS > 2) load(stage1);
+  if constexpr (NS > 3) load(stage2);
+  // One slice, in `cur`; `free` held the one before.
+  auto step = [&](char* cur, char* free) {
+    wait_and_meet<(NS - 2) * Tile::LOADS>();  // the slice is in LDS, and every wave has read the one before
+    load(free);
     F.template read<0>(cur, wm, wn, lane);
     F.template mma<0>(acc);
     F.template read<1>(cur, wm, wn, lane);
     F.template mma<1>(acc);
   };
-  for (int k = k0; k < kend; k += 2 * BKE) {  // a slice past the end is zeros
-    step(stage0, stage1);
+  int slices = (kend - k0 + BKE - 1) / BKE;
+  for (; slices >= NS; slices -= NS) {
+    step(stage0, NS == 2 ? stage1 : NS == 3 ? stage2 : stage3);
     step(stage1, stage0);
+    if constexpr (NS > 2) step(stage2, stage1);
+    if constexpr (NS > 3) step(stage3, stage2);
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);
-  __syncthreads();
+  if (slices > 0) step(stage0, NS == 2 ? stage1 : NS == 3 ? stage2 : stage3);
+  if constexpr (NS > 2)
+    if (slices > 1) step(stage1, stage0);
+  if constexpr (NS > 3)
+    if (slices > 2) step(stage2, stage1);
+  wait_and_meet<0>();
 
   // a lane's columns are the same in every row it finishes
   constexpr int LPR = Tile::TN / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
@@ -429,6 +459,11 @@ __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) 
   float* part = P.part + ((int64_t)split * P.cells + c) * P.M * P.part_ld;
 #pragma unroll
   for (int h = 0; h < Tile::TM / Tile::ER; ++h) {
+    constexpr int PASSES = Tile::ER / RPP;
+    const int mh = m0 + wm + h * Tile::ER + lane / LPR;
+    typename Vec8<T>::type r[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) r[p] = residual8<T>(P.f, c, mh + p * RPP, n, mh + p * RPP < P.M ? left : 0);
     if (h) __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < Tile::ER / 16; ++i)
@@ -438,14 +473,15 @@ __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) 
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    for (int p = 0; p < Tile::ER / RPP; ++p) {
-      const int row = p * RPP + lane / LPR, m = m0 + wm + h * Tile::ER + row;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int row = p * RPP + lane / LPR, m = mh + p * RPP;
       if (m >= P.M || left <= 0) continue;
       const f32x4 lo = *(const f32x4*)(mine + row * Tile::EP + 8 * (lane % LPR));
       const f32x4 hi = *(const f32x4*)(mine + row * Tile::EP + 8 * (lane % LPR) + 4);
       const f32x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       if (sums) store8(part + (int64_t)m * P.part_ld + n, 8, v);
-      else finish8<T>(P.f, c, m, n, left, v, bias, ws);
+      else finish8<T>(P.f, c, m, n, left, v, bias, ws, r[p]);
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   }
@@ -469,7 +505,7 @@ __global__ __launch_bounds__(256) void join_splits_kernel(const GemmArgs P) {
     for (int e = 0; e < 8; ++e) v[e] += w[e];
   }
   finish8<T>(P.f, c, m, n, left, v, column8(P.f.bias, P.f.bias_cell, c, n, left),
-             column8(P.f.ws, P.f.ws_cell, c, n, left));
+             column8(P.f.ws, P.f.ws_cell, c, n, left), residual8<T>(P.f, c, m, n, left));
 }
 
 // ---- the host's checks, operands and workspaces ----

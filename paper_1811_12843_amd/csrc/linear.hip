@@ -21,33 +21,44 @@ struct SlopeArgs {
   float slope;
 };
 
-// 32 lanes x 8 columns, 8 rows at a time
+// 32 lanes x 8 columns, 8 rows at a time; four of a thread's rows in flight.
 template <class T>
 __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs P) {
+  using Raw = typename Vec8<T>::type;
   __shared__ float sums[8][256 + 8];
   const int c = blockIdx.z, lane = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int n = blockIdx.x * 256 + 8 * lane, left = P.N - n, m0 = blockIdx.y * kRowsPer;
+  const int n = blockIdx.x * 256 + 8 * lane, left = P.N - n, m0 = blockIdx.y * kRowsPer + r;
+  const bool slopes = P.act != LIPZ_ACT_LINEAR;
   f32x8 s = {};
   if (left > 0 || (P.dz && n < P.dz_ld)) {
-#pragma unroll 4
-    for (int i = 0; i < kRowsPer / 8; ++i) {
-      const int m = m0 + 8 * i + r;
-      if (m >= P.M) break;
-      f32x8 d = load8((const T*)P.dy + c * P.dy_cell + m * P.dy_ld + n, left);
-      if (P.act != LIPZ_ACT_LINEAR && left > 0) {
-        const f32x8 z = load8((const T*)P.pre + c * P.pre_cell + m * P.pre_ld + n, left);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] *= act_slope<(sizeof(T) < 4)>(P.act, z[e], P.slope);
+    for (int i0 = 0; i0 < kRowsPer / 8; i0 += 4) {
+      Raw d[4], z[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = m0 + 8 * (i0 + i), in = m < P.M ? left : 0;
+        d[i] = load8_raw((const T*)P.dy + c * P.dy_cell + m * P.dy_ld + n, in);
+        z[i] = slopes ? load8_raw((const T*)P.pre + c * P.pre_cell + m * P.pre_ld + n, in) : Raw{};
       }
-      if (P.dz) {
-        if (left < 8) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) d[e] = e < left ? d[e] : 0.f;
+      for (int i = 0; i < 4; ++i) {
+        const int m = m0 + 8 * (i0 + i);
+        f32x8 v = widen<T>(d[i]);
+        if (slopes) {
+          const f32x8 w = widen<T>(z[i]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= act_slope<(sizeof(T) < 4)>(P.act, w[e], P.slope);
+          if (left < 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < left ? v[e] : 0.f;
+          }
         }
-        store8((T*)P.dz + c * P.dz_cell + m * P.dz_ld + n, 8, d);
-      }
+        if (m < P.M) {
+          if (P.dz) store8((T*)P.dz + c * P.dz_cell + m * P.dz_ld + n, 8, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] += d[e];
+          for (int e = 0; e < 8; ++e) s[e] += v[e];
+        }
+      }
     }
   }
   if (!P.part) return;

@@ -4,8 +4,8 @@
 //
 // The quantiser turns w [fan_in][fan_out] into rows of fan_in bytes, so that the
 // product reads both operands along k.  Two launches: column maxima per block
-// of rows, then, per 64 x 64 tile, the column's scale from those and the tile
-// through LDS, each wave writing whole rows of 64 bytes.  Bound by memory: w is
+// of rows, then, per 128 x 64 tile, the column's scale from those and the tile
+// through LDS, 16 lanes writing 128 bytes of a row.  Bound by memory: w is
 // read twice, the second time mostly from the Infinity Cache.
 #include "block_gemm.h"
 
@@ -26,21 +26,28 @@ struct QuantArgs {
   int K, N;
 };
 
-// 32 lanes x 8 columns, 8 rows at a time
+// 32 lanes x 8 columns, 8 rows at a time; eight of a thread's rows in flight.
 template <class T>
 __global__ __launch_bounds__(256) void column_max_kernel(const QuantArgs P) {
+  using Raw = typename Vec8<T>::type;
   __shared__ float top[8][256 + 8];
   const int c = blockIdx.z, lane = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int n = blockIdx.x * 256 + 8 * lane, left = P.N - n, k0 = blockIdx.y * kMaxRowsPer;
+  const int n = blockIdx.x * 256 + 8 * lane, left = P.N - n, k0 = blockIdx.y * kMaxRowsPer + r;
   f32x8 m = {};
   if (left > 0) {
-#pragma unroll 4
-    for (int i = 0; i < kMaxRowsPer / 8; ++i) {
-      const int k = k0 + 8 * i + r;
-      if (k >= P.K) break;
-      const f32x8 v = load8((const T*)P.w + c * P.w_cell + k * P.w_ld + n, left);
+    for (int i0 = 0; i0 < kMaxRowsPer / 8; i0 += 8) {
+      Raw v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m[e] = max_nan(m[e], __builtin_fabsf(v[e]));
+      for (int i = 0; i < 8; ++i) {
+        const int k = k0 + 8 * (i0 + i);
+        v[i] = load8_raw((const T*)P.w + c * P.w_cell + k * P.w_ld + n, k < P.K ? left : 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const f32x8 x = widen<T>(v[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[e] = max_nan(m[e], __builtin_fabsf(x[e]));
+      }
     }
   }
 #pragma unroll
@@ -54,37 +61,53 @@ __global__ __launch_bounds__(256) void column_max_kernel(const QuantArgs P) {
   P.part[((int64_t)c * gridDim.y + blockIdx.y) * P.N + col] = t;
 }
 
+// A block turns 128 rows x 64 columns.  LDS holds them as rows of w, in chunks
+// of 8 columns whose place is xored with the row's 8-row group, so that the
+// reads down a column by lanes 8 rows apart lie on different banks.
+constexpr int kQuantRows = 128;
 template <class T>
 __global__ __launch_bounds__(256) void quantize_kernel(const QuantArgs P) {
-  __shared__ float tile[64][64 + 1], scale[64];
-  const int c = blockIdx.z, n0 = blockIdx.x * 64, k0 = blockIdx.y * 64, t = threadIdx.x;
+  using Raw = typename Vec8<T>::type;
+  __shared__ float top[4][64], scale[64];
+  __shared__ __attribute__((aligned(16))) T tile[kQuantRows][64];
+  const int c = blockIdx.z, n0 = blockIdx.x * 64, k0 = blockIdx.y * kQuantRows, t = threadIdx.x;
   const int chunks = (P.K + kMaxRowsPer - 1) / kMaxRowsPer;
-  if (t < 64 && n0 + t < P.N) {
-    const LIPZ_GLOBAL float* p = as_global(P.part) + (int64_t)c * chunks * P.N + n0 + t;
-    float m = 0.f;
-    for (int i = 0; i < chunks; ++i) m = max_nan(m, p[(int64_t)i * P.N]);
-    scale[t] = fp8_scale(m);
-    if (blockIdx.y == 0) P.scale[c * P.scale_cell + n0 + t] = scale[t];
+  const int x = t & 7, left = P.N - n0 - 8 * x;
+  Raw v[kQuantRows / 32];
+#pragma unroll
+  for (int i = 0; i < kQuantRows / 32; ++i) {
+    const int k = k0 + 32 * i + (t >> 3);
+    v[i] = load8_raw((const T*)P.w + c * P.w_cell + k * P.w_ld + n0 + 8 * x, k < P.K ? left : 0);
   }
-  const int col = 8 * (t & 7), left = P.N - n0 - col;
+  {
+    const int col = t & 63, g = t >> 6;
+    const LIPZ_GLOBAL float* p = as_global(P.part) + (int64_t)c * chunks * P.N + n0 + col;
+    float m = 0.f;
+    if (n0 + col < P.N) {
+#pragma unroll 8
+      for (int i = g; i < chunks; i += 4) m = max_nan(m, p[(int64_t)i * P.N]);
+    }
+    top[g][col] = m;
+  }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int k = 32 * i + (t >> 3);
-    const f32x8 v = k0 + k < P.K && left > 0
-                        ? load8((const T*)P.w + c * P.w_cell + (k0 + k) * P.w_ld + n0 + col, left)
-                        : f32x8{};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) tile[k][col + e] = v[e];
+  for (int i = 0; i < kQuantRows / 32; ++i) {
+    const int row = 32 * i + (t >> 3);
+    *(Raw*)&tile[row][8 * (x ^ ((row >> 3) & 7))] = v[i];
+  }
+  __syncthreads();
+  if (t < 64) {
+    scale[t] = fp8_scale(max_nan(max_nan(top[0][t], top[1][t]), max_nan(top[2][t], top[3][t])));
+    if (blockIdx.y == 0 && n0 + t < P.N) P.scale[c * P.scale_cell + n0 + t] = scale[t];
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int n = 32 * i + (t >> 3), k = 8 * (t & 7);
+  for (int i = 0; i < kQuantRows / 32; ++i) {
+    const int k = 8 * (t & 15), n = 16 * i + (t >> 4);  // 16 lanes write a row's 128 bytes
     if (n0 + n >= P.N || k0 + k >= P.K) continue;
-    f32x8 v;
+    f32x8 o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = tile[k + e][n] / scale[n];
-    store8_fp8(P.q + c * P.q_cell + (n0 + n) * P.q_ld + k0 + k, P.K - k0 - k, v);
+    for (int e = 0; e < 8; ++e) o[e] = (float)tile[k + e][8 * ((n >> 3) ^ (t & 7)) + (n & 7)] / scale[n];
+    store8_fp8(P.q + c * P.q_cell + (n0 + n) * P.q_ld + k0 + k, P.K - k0 - k, o);
   }
 }
 
@@ -123,7 +146,7 @@ size_t quant_bytes(const lipz_quantize_weights_args* a) {
 template <class T>
 void run_quant(const QuantArgs& P, int cells, hipStream_t s) {
   column_max_kernel<T><<<dim3(tiles_of(P.N, 256), tiles_of(P.K, kMaxRowsPer), cells), 256, 0, s>>>(P);
-  quantize_kernel<T><<<dim3(tiles_of(P.N, 64), tiles_of(P.K, 64), cells), 256, 0, s>>>(P);
+  quantize_kernel<T><<<dim3(tiles_of(P.N, 64), tiles_of(P.K, kQuantRows), cells), 256, 0, s>>>(P);
 }
 
 struct Fp8Layout {

@@ -215,32 +215,36 @@ __global__ __launch_bounds__(Group<TPR>::NT) void rms_norm_bwd_kernel(const Norm
     const T* yp = (const T*)P.dy + c * P.dy_cell + row * P.dy_ld;
     const T* rp = P.dh ? (const T*)P.dh + c * P.dh_cell + row * P.dh_ld : nullptr;
     const float rstd = as_global(P.rstd)[(int64_t)c * P.rows + row];
-    f32x8 xh[NV], u[NV], add[NV];
+    typename Vec8<T>::type h[NV], dy[NV], dh[NV];  // converted twice rather than held in fp32
     float s = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = 8 * (v * TPR + t);
-      const bool in = col < P.cols;
-      xh[v] = in ? load8(hp + col, P.cols - col) : f32x8{};
-      u[v] = in ? load8(yp + col, P.cols - col) : f32x8{};
-      add[v] = in && rp ? load8(rp + col, P.cols - col) : f32x8{};
+      const int col = 8 * (v * TPR + t), n = P.cols - col;
+      h[v] = n > 0 ? load8_raw(hp + col, n) : typename Vec8<T>::type{};
+      dy[v] = n > 0 ? load8_raw(yp + col, n) : typename Vec8<T>::type{};
+      dh[v] = n > 0 && rp ? load8_raw(rp + col, n) : typename Vec8<T>::type{};
     }
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+      const f32x8 x = widen<T>(h[v]), d = widen<T>(dy[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        xh[v][e] *= rstd;
-        dg[v][e] = fmaf(u[v][e], xh[v][e], dg[v][e]);
-        u[v][e] *= gm[v][e];
-        s = fmaf(u[v][e], xh[v][e], s);
+        const float xh = x[e] * rstd;
+        dg[v][e] = fmaf(d[e], xh, dg[v][e]);
+        s = fmaf(d[e] * gm[v][e], xh, s);
       }
+    }
     const float mean = G::all(s, red, turn, Add()) / (float)P.cols;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int col = 8 * (v * TPR + t);
+      forget(h[v]);
+      forget(dy[v]);
+      const f32x8 x = widen<T>(h[v]), d = widen<T>(dy[v]), r = widen<T>(dh[v]);
+      f32x8 o;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) u[v][e] = fmaf(rstd, fmaf(-xh[v][e], mean, u[v][e]), add[v][e]);
-      if (col < P.cols) store8((T*)P.dx + c * P.dx_cell + row * P.dx_ld + col, P.cols - col, u[v]);
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(rstd, fmaf(-(x[e] * rstd), mean, d[e] * gm[v][e]), r[e]);
+      if (col < P.cols) store8((T*)P.dx + c * P.dx_cell + row * P.dx_ld + col, P.cols - col, o);
     }
   }
   if (!P.part) return;
@@ -311,22 +315,34 @@ __global__ __launch_bounds__(1024) void rms_norm_bwd_long_kernel(const NormBwdAr
 
 }  // namespace
 
-// out[c][col] = sum over the n rows of part[c], in order; four rows in flight.
+// out[c][col] = sum over the n rows of part[c]: 16 columns a block, 16 threads a
+// column, thread g the rows g, g + 16, .. (eight in flight); then theirs in order.
 __global__ __launch_bounds__(256) void sum_parts_kernel(const float* part, int n, int cols, float* out, int64_t out_cell) {
-  const int col = blockIdx.x * 256 + threadIdx.x, c = blockIdx.y;
-  if (col >= cols) return;
+  __shared__ float sums[16][16 + 1];
+  const int lane = threadIdx.x & 15, g = threadIdx.x >> 4, col = blockIdx.x * 16 + lane, c = blockIdx.y;
   const LIPZ_GLOBAL float* p = as_global(part) + (int64_t)c * n * cols + col;
-  float s[4] = {};
-  int i = 0;
-  for (; i + 4 <= n; i += 4)
+  float s = 0.f;
+  if (col < cols) {
+    int i = g;
+    for (; i + 112 < n; i += 128) {
+      float v[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) s[u] += p[(int64_t)(i + u) * cols];
-  for (; i < n; ++i) s[0] += p[(int64_t)i * cols];
-  as_global(out)[c * out_cell + col] = (s[0] + s[1]) + (s[2] + s[3]);
+      for (int u = 0; u < 8; ++u) v[u] = p[(int64_t)(i + 16 * u) * cols];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; i < n; i += 16) s += p[(int64_t)i * cols];
+  }
+  sums[g][lane] = s;
+  __syncthreads();
+  if (g || col >= cols) return;
+#pragma unroll
+  for (int q = 1; q < 16; ++q) s += sums[q][lane];
+  as_global(out)[c * out_cell + col] = s;
 }
 
 hipError_t launch_sum_parts(const float* part, int n, int cols, int cells, float* out, int64_t out_cell, hipStream_t s) {
-  sum_parts_kernel<<<dim3((cols + 255) / 256, cells), 256, 0, s>>>(part, n, cols, out, out_cell);
+  sum_parts_kernel<<<dim3((cols + 15) / 16, cells), 256, 0, s>>>(part, n, cols, out, out_cell);
   return hipGetLastError();
 }
 
