@@ -6,13 +6,21 @@
 // An operand is KC (k contiguous: A [M][K] or B stored [N][K]) or KM (k is the
 // row: A stored [K][M], B [K][N]).
 //
-// A workgroup owns a BM x BN tile and walks K in slices of 128 bytes per row
-// (32 k of fp32, 64 of 16 bits, 128 of e4m3) through NS LDS stages, NS - 1 slices
-// in flight ahead of the one that is multiplied; one barrier per slice.
+// A workgroup owns a BM x BN tile and walks K in slices of SB bytes per row
+// through NS LDS stages.  A slice is multiplied in two parts: the second part's
+// fragments are read before the first one's MFMAs and the next slice's first
+// ones before the second's; one barrier per slice, between the parts, after
+// which every wave holds the slice in registers and its stage takes the slice
+// NS on.  Tiles of 64 and 128 rows: SB = 128 (32 k of fp32, 64 of 16 bits, 128 of
+// e4m3); of 256 rows: SB = 64.  MFMAs are 16 x 16 (one 16 x 16 x 32 moves less
+// between registers than a 32 x 32 x 16, and the card's power is what bounds
+// large products: 8192 x 4096 x 4096 bf16 along k 212 and 229 us), for e4m3 on
+// large tiles 32 x 32 x 64.
 //
 // LDS.  KC: a row of 128 bytes is eight 16-byte chunks, chunk c at place
-// c ^ (row % 8), so that the 16 rows that a fragment read touches lie on all
-// banks.  KM: rows of the tile's columns; the chunk index is xored with bits
+// c ^ (row % 8) (of 64 bytes four, at c ^ (-(row / 4) % 4)): a 16-byte read serves
+// lanes 0-3, 12-15, 20-23 and 24-27 together, and so on, and their rows then lie
+// on all banks.  KM: rows of the tile's columns; the chunk index is xored with bits
 // of k (km_swizzle), so that the k rows that a transposing read (16 bits) or
 // four b32 reads (fp32) touch lie on different banks.  Lanes permute the
 // global chunk they fetch, not the LDS address: loads go straight into LDS.
@@ -43,7 +51,15 @@ struct Fp8Wide {};
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_any;
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+template <class V>
+__device__ __forceinline__ V lds_get(const lds_char* p) {
+  return *(const __attribute__((address_space(3))) V*)p;
+}
 
 template <class E>
 struct ElemSize {
@@ -78,7 +94,6 @@ struct GemmArgs {
   Finish f;
 };
 
-constexpr int kSlice = 128;  // bytes of a row in a slice
 constexpr uint32_t kPast = 0x80000000u;
 
 // ---- finishing: 8 columns of a row from column n on, `left` of them inside ----
@@ -98,10 +113,7 @@ __device__ __forceinline__ void finish8(const Finish& f, int c, int m, int n, in
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += bias[e];
   if (f.pre) store8((T*)f.pre + c * f.pre_cell + m * f.pre_ld + n, left, v);
-  if (f.act != LIPZ_ACT_LINEAR) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_of<FAST>(f.act, v[e], f.slope);
-  }
+  v = act8<FAST>(f.act, v, f.slope);
   if (f.r) {
     const f32x8 r = widen<T>(residual);
 #pragma unroll
@@ -116,27 +128,34 @@ __device__ __forceinline__ f32x8 column8(const float* p, int64_t cell, int c, in
 // ---- operands ----
 
 // The place of chunk x (16 bytes) of k row k in a KM tile of R columns is
-// x ^ km_swizzle(k).  16 bits: a transposing read takes 32 bytes of each of
-// the k rows 8 g + 0 .. 3 (or 4 .. 7), g the lane's group of 16; two groups
-// are served at a time.  fp32: a read takes 64 bytes of k rows 4 g + u.
-template <int ES, int R>
+// x ^ km_swizzle(k); MF: the MFMA's rows.  16 bits: a transposing read of a
+// group of 16 lanes takes 32 bytes of each of four k rows; two groups are
+// served at a time: other k rows, 8 on (MF = 16), or the next 32 bytes of the
+// same (MF = 32).  fp32: a read takes 64 bytes of k rows 4 g + u.
+template <int ES, int R, int MF>
 __device__ __forceinline__ int km_swizzle(int k) {
   if (ES == 4) return 4 * ((k >> 2) & 3);
+  if (MF == 32) return 4 * (k & 3);
   if (R * ES >= 256) return 2 * ((k & 3) | ((k >> 1) & 4));
   return 2 * (((k >> 1) & 1) | ((k >> 2) & 2));
 }
+template <int SB>
+__device__ __forceinline__ int kc_swizzle(int row) {
+  return SB == 128 ? row & 7 : -(row >> 2) & 3;
+}
 
-template <int ES, bool KC, int R, int NT>
+template <int ES, bool KC, int R, class Tile>
 struct Operand {
-  static constexpr int EPC = 16 / ES, BKE = kSlice / ES;
-  static constexpr int NI = R * 8 / NT;             // chunks of a slice per thread
-  static constexpr int CPR = KC ? 8 : R * ES / 16;  // chunks of an LDS row
+  static constexpr int SB = Tile::SB, NT = Tile::NT;
+  static constexpr int EPC = 16 / ES, BKE = SB / ES;
+  static constexpr int NI = R * SB / 16 / NT;             // chunks of a slice per thread
+  static constexpr int CPR = KC ? SB / 16 : R * ES / 16;  // chunks of an LDS row
   const char* base;  // the next slice of the tile
   int64_t step;      // bytes per slice
   int extent;        // KC: bytes from base to the end of the tile's last row; KM: bytes of the operand's columns from the tile's on
   int ld;            // KM: row pitch
   int kleft;         // k left from the next slice on
-  uint32_t off[NI];  // the thread's chunks, from base
+  uint32_t off[NI];  // the thread's chunks in a slice, from its base
   int k;             // KC: first k of the thread's chunks in their slice (the same in all of them)
 
   __device__ __forceinline__ void init(const char* p, int64_t ld_bytes, int rc0, int rc_all, int K, int k0) {
@@ -144,23 +163,24 @@ struct Operand {
     kleft = K - k0;
     if (KC) {
       base = p + (int64_t)rc0 * ld_bytes + (int64_t)k0 * ES;
-      step = kSlice;
+      step = SB;
       extent = (min(rc_all - rc0, R) - 1) * ld + (kleft * ES + 15) / 16 * 16;  // (packed rows end in zeros)
     } else {
       base = p + (int64_t)k0 * ld_bytes + (int64_t)rc0 * ES;
       step = BKE * ld_bytes;
       extent = ((rc_all - rc0) * ES + 3) / 4 * 4;
     }
+    static_assert(!KC || NT / CPR % 16 == 0, "a thread's rows have the same swizzle");
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int q = i * NT + (int)threadIdx.x, row = q / CPR, at = q % CPR;
-      const int x = KC ? at ^ (row & 7) : at ^ km_swizzle<ES, R>(row);
+      const int x = at ^ (KC ? kc_swizzle<SB>(row) : km_swizzle<ES, R, Tile::MF>(row));
       off[i] = (uint32_t)row * (uint32_t)ld + x * 16;
       if (KC) k = x * EPC;
     }
   }
   // The next slice into LDS; one past the end of K is zeros.
-  __device__ __forceinline__ void load(char* st) {
+  __device__ __forceinline__ void load(lds_char* st) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // (no branches here: with one, the compiler no longer sees which stage a
     // load in flight goes to, and waits for it before it reads the other)
@@ -173,7 +193,7 @@ struct Operand {
     }
     base += step;
     kleft -= BKE;
-    if (KC) extent -= kSlice;
+    if (KC) extent -= SB;
   }
 };
 
@@ -181,20 +201,20 @@ struct Operand {
 // row l % 16 and, of the slice's half kk, 16 bytes of k (16 bits: k = 32 kk +
 // 8 (l / 16) .. + 7; fp32: 16 kk + 4 (l / 16) .. + 3; e4m3: 64 kk + 16 (l / 16) .. +
 // 15; A and B need only agree).  N of them, 16 rows apart.
-template <int ES, bool KC, int R, int N>
+template <int ES, bool KC, int R, int MF, int SB, int N>
 struct Fragments {
-  static __device__ __forceinline__ void read(const char* st, int r0, int kk, int lane, u32x4* out) {
+  static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
     const int li = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = r0 + 16 * i + li;
       if (KC) {
-        out[i] = *(const u32x4*)(st + r * kSlice + (((4 * kk + g) ^ (li & 7)) << 4));
+        out[i] = lds_get<u32x4>(st + r * SB + (((4 * kk + g) ^ kc_swizzle<SB>(li)) << 4));
       } else {  // fp32
         const int k = 16 * kk + 4 * g;
-        const char* p = st + k * (R * 4) + (((r >> 2) ^ km_swizzle<4, R>(k)) << 4) + 4 * (r & 3);
+        const lds_char* p = st + k * (R * 4) + (((r >> 2) ^ km_swizzle<4, R, 16>(k)) << 4) + 4 * (r & 3);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) out[i][u] = *(const uint32_t*)(p + u * (R * 4));
+        for (int u = 0; u < 4; ++u) out[i][u] = lds_get<uint32_t>(p + u * (R * 4));
       }
     }
   }
@@ -202,36 +222,55 @@ struct Fragments {
 
 // 16 bits, KM, by transposing reads: in each, lane i of a group of 16 gives the
 // address of four columns of k row i / 4 and receives column i of the four
-// rows.  In assembly, two fragments at a time and waited for there: the
-// compiler does not tell which stage such a read goes to, and would wait for
-// the loads in flight to the other one first.
-__device__ __forceinline__ uint32_t lds_offset(const char* p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+// rows; a second one takes the k rows 4 on.  The two index the stage each by
+// itself: the compiler follows a pointer only some steps to see which stage it
+// reads, and waits for every load in flight where it no longer sees it.
+__device__ __forceinline__ u32x4 read_transposed(const lds_char* st, int at, int at4) {
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  typedef short v8s __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) v4s lds_v4s;
+  const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(st + at));
+  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(st + at4));
+  return __builtin_bit_cast(u32x4, (v8s{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}));
 }
-template <int R, int N>
-struct Fragments<2, false, R, N> {
-  static __device__ __forceinline__ void read(const char* st, int r0, int kk, int lane, u32x4* out) {
-    static_assert(N % 2 == 0, "pairs of fragments");
-    const int li = lane & 15, g = lane >> 4;
-    const int k = 8 * g + (li >> 2);
-    const uint32_t p = lds_offset(st) + k * (R * 2) + 8 * (li & 1);
-    const int x = (r0 >> 3) + ((li >> 1) & 1), w = km_swizzle<2, R>(k);
+__device__ __forceinline__ int hidden(int v) {
+  asm("" : "+v"(v));
+  return v;
+}
+template <int R, int SB, int N>
+struct Fragments<2, false, R, 16, SB, N> {
+  static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
+    const int li = lane & 15, k = 8 * (lane >> 4) + (li >> 2);
+    const int p = k * (R * 2) + 8 * (li & 1), p4 = hidden(p + 4 * R * 2);
+    const int x = (r0 >> 3) + ((li >> 1) & 1), w = km_swizzle<2, R, 16>(k);
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      u32x2 a, b, c, d;
-      asm volatile(
-          "ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
-          "ds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-          "ds_read_b64_tr_b16 %2, %5 offset:%6\n\t"
-          "ds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
-          "s_waitcnt lgkmcnt(0)"
-          : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
-          : "v"(p + (((x + 2 * i) ^ w) << 4)), "v"(p + (((x + 2 * i + 2) ^ w) << 4)), "i"(kk * 32 * R * 2),
-            "i"((kk * 32 + 4) * R * 2)
-          : "memory");
-      out[i] = u32x4{a[0], a[1], b[0], b[1]};
-      out[i + 1] = u32x4{c[0], c[1], d[0], d[1]};
-    }
+    for (int i = 0; i < N; ++i)
+      out[i] = read_transposed(st, p + (((x + 2 * i) ^ w) << 4) + kk * 32 * R * 2,
+                               p4 + (((x + 2 * i) ^ w) << 4) + kk * 32 * R * 2);
+  }
+};
+
+// For 32 x 32 MFMAs, slices of 64 bytes: lane l holds row l % 32; 16 bits: k = 16 kk +
+// 8 (l / 32) .. + 7; e4m3 (whole slices): chunks l / 32 and 2 + l / 32.
+template <int ES, int R, int N>
+struct Fragments<ES, true, R, 32, 64, N> {
+  static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
+    const int li = lane & 31, g = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      out[i] = lds_get<u32x4>(st + (r0 + 32 * i + li) * 64 + (((2 * kk + g) ^ kc_swizzle<64>(li)) << 4));
+  }
+};
+template <int R, int N>
+struct Fragments<2, false, R, 32, 64, N> {
+  static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
+    const int li = lane & 15, k = 8 * (lane >> 5) + (li >> 2);
+    const int p = k * (R * 2) + 8 * (li & 1), p4 = hidden(p + 4 * R * 2);
+    const int x = (r0 >> 3) + 2 * ((lane >> 4) & 1) + ((li >> 1) & 1), w = km_swizzle<2, R, 32>(k);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      out[i] = read_transposed(st, p + (((x + 4 * i) ^ w) << 4) + kk * 16 * R * 2,
+                               p4 + (((x + 4 * i) ^ w) << 4) + kk * 16 * R * 2);
   }
 };
 
@@ -242,11 +281,17 @@ struct Mma<__bf16> {
   static __device__ __forceinline__ f32x4 run(u32x4 b, u32x4 a, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
   }
+  static __device__ __forceinline__ f32x16 run(u32x4 b, u32x4 a, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+  }
 };
 template <>
 struct Mma<_Float16> {
   static __device__ __forceinline__ f32x4 run(u32x4 b, u32x4 a, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 run(u32x4 b, u32x4 a, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
   }
 };
 template <>
@@ -261,27 +306,21 @@ struct Mma<float> {
 
 // ---- tiles ----
 
-#ifndef LIPZ_NS_S
-#define LIPZ_NS_S 4
-#endif
-#ifndef LIPZ_NS_M
-#define LIPZ_NS_M 4
-#endif
-template <int BM_, int BN_, int WM_, int WN_, int NS_>
+template <int BM_, int BN_, int WM_, int WN_, int NS_, int SB_, int MF_>
 struct TileShape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;  // WM x WN waves
-  static constexpr int NS = NS_;                                // LDS stages
+  static constexpr int NS = NS_, SB = SB_, MF = MF_;            // LDS stages, bytes of a slice's row, MFMA's rows
   static constexpr int NT = 64 * WM * WN, TM = BM / WM, TN = BN / WN;
-  static constexpr int MI = TM / 16, NI = TN / 16;
-  static constexpr int A_BYTES = BM * kSlice, STAGE = A_BYTES + BN * kSlice;
-  static constexpr int LOADS = STAGE / 16 / NT;  // of a slice, per wave
-  static constexpr int ER = 32;                  // rows of a wave's block that pass through LDS at a time
-  static constexpr int EP = TN + 4;              // their pitch in floats
-  static_assert(WM * WN / 2 * ER * EP * 4 <= STAGE, "a stage holds half of the waves' rows");
+  static constexpr int MI = TM / MF, NI = TN / MF;
+  static constexpr int A_BYTES = BM * SB, B_BYTES = BN * SB;
+  static constexpr int LOADS = (A_BYTES + B_BYTES) / 16 / NT;  // of a slice, per wave
+  static_assert(NS >= 2 && NS <= 4 && 2 * NS >= WM * WN && TM % 32 == 0 && TN % 32 == 0 && BM * SB >= 4096);
+  typedef std::conditional_t<MF == 16, f32x4, f32x16> Acc;
 };
-typedef TileShape<64, 64, 2, 2, LIPZ_NS_S> TileS;
-typedef TileShape<128, 128, 2, 2, LIPZ_NS_M> TileM;
-typedef TileShape<256, 256, 2, 4, 2> TileL;
+typedef TileShape<64, 64, 2, 2, 4, 128, 16> TileS;
+typedef TileShape<128, 128, 2, 2, 4, 128, 16> TileM;
+template <class E>
+using TileL = TileShape<256, 256, 2, 4, 4, 64, std::is_same_v<E, Fp8Wide> ? 32 : 16>;
 
 // Waits until all but this wave's last n vector loads have landed and its LDS
 // accesses are done, then for the other waves.  No more than that: the
@@ -294,22 +333,45 @@ __device__ __forceinline__ void wait_and_meet() {
   asm volatile("" ::: "memory");
 }
 
-// A wave's products of a slice, in two parts.  16 bits and fp32: a part is half
-// the slice's k.
-template <class E, bool AKC, bool BKC, class Tile>
+// A wave's products of a slice, in two parts.  Where MFMAs take the slice's k
+// in one step, a part is half of the wave's rows.
+template <class E, bool AKC, bool BKC, class Tile, bool ONE_STEP>
 struct Parts {
+  static constexpr int ES = ElemSize<E>::value, H = Tile::MI / 2;
+  u32x4 a[2][H], b[2][Tile::NI];  // B's serve both parts: b[1] are the ones of the part that is left
+  __device__ __forceinline__ void turn() {
+#pragma unroll
+    for (int j = 0; j < Tile::NI; ++j) b[1][j] = b[0][j];
+  }
+  template <int P>
+  __device__ __forceinline__ void read(const lds_char* sa, const lds_char* sb, int wm, int wn, int lane) {
+    if (P == 0) Fragments<ES, BKC, Tile::BN, Tile::MF, Tile::SB, Tile::NI>::read(sb, wn, 0, lane, b[0]);
+    Fragments<ES, AKC, Tile::BM, Tile::MF, Tile::SB, H>::read(sa, wm + Tile::MF * H * P, 0, lane, a[P]);
+  }
+  template <int P>
+  __device__ __forceinline__ void mma(typename Tile::Acc (&acc)[Tile::MI][Tile::NI]) {
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+#pragma unroll
+      for (int j = 0; j < Tile::NI; ++j) acc[H * P + i][j] = Mma<E>::run(b[P][j], a[P][i], acc[H * P + i][j]);
+  }
+};
+// Otherwise (16 bits and fp32) half of its k.
+template <class E, bool AKC, bool BKC, class Tile>
+struct Parts<E, AKC, BKC, Tile, false> {
   static constexpr int ES = ElemSize<E>::value;
   struct Frag {
     u32x4 a[Tile::MI], b[Tile::NI];
   };
   Frag f[2];
+  __device__ __forceinline__ void turn() {}
   template <int P>
-  __device__ __forceinline__ void read(const char* st, int wm, int wn, int lane) {
-    Fragments<ES, BKC, Tile::BN, Tile::NI>::read(st + Tile::A_BYTES, wn, P, lane, f[P].b);
-    Fragments<ES, AKC, Tile::BM, Tile::MI>::read(st, wm, P, lane, f[P].a);
+  __device__ __forceinline__ void read(const lds_char* sa, const lds_char* sb, int wm, int wn, int lane) {
+    Fragments<ES, BKC, Tile::BN, Tile::MF, Tile::SB, Tile::NI>::read(sb, wn, P, lane, f[P].b);
+    Fragments<ES, AKC, Tile::BM, Tile::MF, Tile::SB, Tile::MI>::read(sa, wm, P, lane, f[P].a);
   }
   template <int P>
-  __device__ __forceinline__ void mma(f32x4 (&acc)[Tile::MI][Tile::NI]) {
+  __device__ __forceinline__ void mma(typename Tile::Acc (&acc)[Tile::MI][Tile::NI]) {
 #pragma unroll
     for (int i = 0; i < Tile::MI; ++i)
 #pragma unroll
@@ -321,25 +383,37 @@ struct Parts {
 template <bool WIDE, class Tile>
 struct Fp8Parts {
   static constexpr int H = Tile::MI / 2;
-  u32x4 b[2][Tile::NI], a[2][H];
+  u32x4 fb[2][2][Tile::NI], fa[2][2][H];  // B's serve both parts: fb[1] are the ones of the part that is left
+  __device__ __forceinline__ void turn() {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int j = 0; j < Tile::NI; ++j) fb[1][kk][j] = fb[0][kk][j];
+  }
   template <int P>
-  __device__ __forceinline__ void read(const char* st, int wm, int wn, int lane) {
+  __device__ __forceinline__ void read(const lds_char* sa, const lds_char* sb, int wm, int wn, int lane) {
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      if (P == 0) Fragments<1, true, Tile::BN, Tile::NI>::read(st + Tile::A_BYTES, wn, kk, lane, b[kk]);
-      Fragments<1, true, Tile::BM, H>::read(st, wm + 16 * H * P, kk, lane, a[kk]);
+      if (P == 0) Fragments<1, true, Tile::BN, Tile::MF, Tile::SB, Tile::NI>::read(sb, wn, kk, lane, fb[0][kk]);
+      Fragments<1, true, Tile::BM, Tile::MF, Tile::SB, H>::read(sa, wm + Tile::MF * H * P, kk, lane, fa[P][kk]);
     }
   }
   template <int P>
-  __device__ __forceinline__ void mma(f32x4 (&acc)[Tile::MI][Tile::NI]) {
+  __device__ __forceinline__ void mma(typename Tile::Acc (&acc)[Tile::MI][Tile::NI]) {
+    const auto& a = fa[P];
+    const auto& b = fb[P];
     if constexpr (WIDE) {
 #pragma unroll
       for (int i = 0; i < H; ++i)
 #pragma unroll
-        for (int j = 0; j < Tile::NI; ++j)
+        for (int j = 0; j < Tile::NI; ++j) {
           // operand formats 0: e4m3; block scales 2^0
-          acc[H * P + i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-              join(b[0][j], b[1][j]), join(a[0][i], a[1][i]), acc[H * P + i][j], 0, 0, 0, 127, 0, 127);
+          const i32x8 w = join(b[0][j], b[1][j]), x = join(a[0][i], a[1][i]);
+          if constexpr (Tile::MF == 16)
+            acc[H * P + i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[H * P + i][j], 0, 0, 0, 127, 0, 127);
+          else
+            acc[H * P + i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc[H * P + i][j], 0, 0, 0, 127, 0, 127);
+        }
     } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -374,9 +448,9 @@ struct Fp8Parts {
   }
 };
 template <bool AKC, bool BKC, class Tile>
-struct Parts<Fp8, AKC, BKC, Tile> : Fp8Parts<false, Tile> {};
+struct Parts<Fp8, AKC, BKC, Tile, false> : Fp8Parts<false, Tile> {};
 template <bool AKC, bool BKC, class Tile>
-struct Parts<Fp8Wide, AKC, BKC, Tile> : Fp8Parts<true, Tile> {};
+struct Parts<Fp8Wide, AKC, BKC, Tile, false> : Fp8Parts<true, Tile> {};
 
 // The tile of a workgroup.  Workgroup b runs on XCD b % 8: each XCD takes a
 // contiguous share of the tiles, and tiles follow each other down `GM` rows
@@ -398,92 +472,140 @@ __device__ __forceinline__ void tile_of(const GemmArgs& P, int GM, int& c, int& 
 
 template <class E, class T, bool AKC, bool BKC, class Tile>
 __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) {
-  constexpr int ES = ElemSize<E>::value, BKE = kSlice / ES;
+  constexpr int ES = ElemSize<E>::value, BKE = Tile::SB / ES;
   // separate arrays: a load into one stage is then seen not to touch the
   // others, and reads of those do not wait for it
   constexpr int NS = Tile::NS;
-  __shared__ __attribute__((aligned(1024))) char stage0[Tile::STAGE], stage1[Tile::STAGE];
-  __shared__ __attribute__((aligned(1024))) char stage2[NS > 2 ? Tile::STAGE : 16], stage3[NS > 3 ? Tile::STAGE : 16];
+  struct Stage {
+    lds_char *a, *b;
+  };
+#define LIPZ_STAGE(i)                                                                               \
+  __shared__ __attribute__((aligned(1024))) char ldsa##i[NS > i ? Tile::A_BYTES : 16];              \
+  __shared__ __attribute__((aligned(1024))) char ldsb##i[NS > i ? Tile::B_BYTES : 16];              \
+  const Stage stage##i = {(lds_char*)ldsa##i, (lds_char*)ldsb##i};
+  LIPZ_STAGE(0)
+  LIPZ_STAGE(1)
+  LIPZ_STAGE(2)
+  LIPZ_STAGE(3)
+#undef LIPZ_STAGE
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / Tile::WN * Tile::TM, wn = wave % Tile::WN * Tile::TN;
   int c, split, tm, tn;
   tile_of(P, 4, c, split, tm, tn);
-  const int m0 = tm * Tile::BM, n0 = tn * Tile::BN;
+  const int m0 = tm * Tile::BM + wm, n0 = tn * Tile::BN + wn;  // the wave's block
   const int k0 = split * P.per_split * BKE, kend = min(P.K, k0 + P.per_split * BKE);
-
-  Operand<ES, AKC, Tile::BM, Tile::NT> A;
-  Operand<ES, BKC, Tile::BN, Tile::NT> B;
-  A.init(P.A + c * P.a_cell, P.a_ld, m0, P.M, kend, k0);
-  B.init(P.B + c * P.b_cell, P.b_ld, n0, P.N, kend, k0);
-  auto load = [&](char* st) {
-    A.load(st);
-    B.load(st + Tile::A_BYTES);
+  Operand<ES, AKC, Tile::BM, Tile> A;
+  Operand<ES, BKC, Tile::BN, Tile> B;
+  A.init(P.A + c * P.a_cell, P.a_ld, tm * Tile::BM, P.M, kend, k0);
+  B.init(P.B + c * P.b_cell, P.b_ld, tn * Tile::BN, P.N, kend, k0);
+  auto load = [&](const Stage& st) {
+    A.load(st.a);
+    B.load(st.b);
   };
-  f32x4 acc[Tile::MI][Tile::NI] = {};
-  Parts<E, AKC, BKC, Tile> F;
   load(stage0);
-  if constexpr (NS > 2) load(stage1);
-  if constexpr (NS > 3) load(stage2);
-  // One slice, in `cur`; `free` held the one before.
-  auto step = [&](char* cur, char* free) {
-    wait_and_meet<(NS - 2) * Tile::LOADS>();  // the slice is in LDS, and every wave has read the one before
-    load(free);
-    F.template read<0>(cur, wm, wn, lane);
-    F.template mma<0>(acc);
-    F.template read<1>(cur, wm, wn, lane);
-    F.template mma<1>(acc);
+  load(stage1);
+  if constexpr (NS > 2) load(stage2);
+  if constexpr (NS > 3) load(stage3);
+  typename Tile::Acc acc[Tile::MI][Tile::NI] = {};
+  Parts<E, AKC, BKC, Tile, ES == 2 && Tile::MF == 16 && Tile::SB == 64> F;
+  // Keeps the order that is written, where registers allow it (both operands
+  // across k take more addresses): 6 cold 8192 x 4096 x 4096 products along k
+  // 1383 us, 1475 in the compiler's order.
+  auto pin = [] {
+    if constexpr (AKC) __builtin_amdgcn_sched_barrier(0);
   };
+  // One slice, in `cur`, its first part's fragments in registers.
+  auto step = [&](const Stage& cur, const Stage& next) {
+    F.template read<1>(cur.a, cur.b, wm, wn, lane);
+    pin();
+    F.template mma<0>(acc);
+    pin();
+    wait_and_meet<(NS - 2) * Tile::LOADS>();  // the next slice is in LDS, and every wave has read this one
+    load(cur);
+    F.turn();
+    F.template read<0>(next.a, next.b, wm, wn, lane);
+    pin();
+    F.template mma<1>(acc);
+    pin();
+  };
+  const Stage& last = NS == 2 ? stage1 : NS == 3 ? stage2 : stage3;
+
   int slices = (kend - k0 + BKE - 1) / BKE;
+  wait_and_meet<(NS - 1) * Tile::LOADS>();
+  F.template read<0>(stage0.a, stage0.b, wm, wn, lane);
   for (; slices >= NS; slices -= NS) {
-    step(stage0, NS == 2 ? stage1 : NS == 3 ? stage2 : stage3);
-    step(stage1, stage0);
-    if constexpr (NS > 2) step(stage2, stage1);
-    if constexpr (NS > 3) step(stage3, stage2);
+    step(stage0, stage1);
+    if constexpr (NS > 2) step(stage1, stage2);
+    if constexpr (NS > 3) step(stage2, stage3);
+    step(last, stage0);
   }
-  if (slices > 0) step(stage0, NS == 2 ? stage1 : NS == 3 ? stage2 : stage3);
+  if (slices > 0) step(stage0, stage1);
   if constexpr (NS > 2)
-    if (slices > 1) step(stage1, stage0);
+    if (slices > 1) step(stage1, stage2);
   if constexpr (NS > 3)
-    if (slices > 2) step(stage2, stage1);
+    if (slices > 2) step(stage2, stage3);
   wait_and_meet<0>();
 
-  // a lane's columns are the same in every row it finishes
-  constexpr int LPR = Tile::TN / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
-  const int li = lane & 15, g = lane >> 4;
-  const int n = n0 + wn + 8 * (lane % LPR), left = P.N - n;
-  constexpr int HALF = Tile::WM * Tile::WN / 2;
-  float* mine = (float*)(wave < HALF ? stage0 : stage1) + (wave % HALF) * (Tile::ER * Tile::EP);
+  // The wave's block, 32 x 32 of it at a time: a lane's columns pass through
+  // LDS, chunk x of a row (16 bytes) at place x ^ (row % 8), and come back as
+  // 8 columns of one row, 16 rows at a time.
   const bool sums = P.splits > 1;
-  const f32x8 bias = sums ? f32x8{} : column8(P.f.bias, P.f.bias_cell, c, n, left);
-  const f32x8 ws = sums ? f32x8{} : column8(P.f.ws, P.f.ws_cell, c, n, left);
   float* part = P.part + ((int64_t)split * P.cells + c) * P.M * P.part_ld;
+  const int at_stage = wave % NS;
+  const Stage& own = at_stage == 0 ? stage0 : at_stage == 1 ? stage1 : at_stage == 2 ? stage2 : stage3;
+  lds_char* mine = wave < NS ? own.a : own.b;
 #pragma unroll
-  for (int h = 0; h < Tile::TM / Tile::ER; ++h) {
-    constexpr int PASSES = Tile::ER / RPP;
-    const int mh = m0 + wm + h * Tile::ER + lane / LPR;
-    typename Vec8<T>::type r[PASSES];
+  for (int bj = 0; bj < Tile::TN / 32; ++bj) {
+    const int n = n0 + 32 * bj + 8 * (lane & 3), left = P.N - n;
+    const f32x8 bias = sums ? f32x8{} : column8(P.f.bias, P.f.bias_cell, c, n, left);
+    const f32x8 ws = sums ? f32x8{} : column8(P.f.ws, P.f.ws_cell, c, n, left);
+    // all of the columns' residuals now: a load is waited for together with the stores before it
+    typename Vec8<T>::type r[Tile::TM / 32][2] = {};
+    if (P.f.r && !sums) {
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) r[p] = residual8<T>(P.f, c, mh + p * RPP, n, mh + p * RPP < P.M ? left : 0);
-    if (h) __builtin_amdgcn_wave_barrier();
+      for (int bi = 0; bi < Tile::TM / 32; ++bi)
 #pragma unroll
-    for (int i = 0; i < Tile::ER / 16; ++i)
-#pragma unroll
-      for (int j = 0; j < Tile::NI; ++j)
-        *(f32x4*)(mine + (16 * i + li) * Tile::EP + 16 * j + 4 * g) = acc[h * (Tile::ER / 16) + i][j];
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      const int row = p * RPP + lane / LPR, m = mh + p * RPP;
-      if (m >= P.M || left <= 0) continue;
-      const f32x4 lo = *(const f32x4*)(mine + row * Tile::EP + 8 * (lane % LPR));
-      const f32x4 hi = *(const f32x4*)(mine + row * Tile::EP + 8 * (lane % LPR) + 4);
-      const f32x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      if (sums) store8(part + (int64_t)m * P.part_ld + n, 8, v);
-      else finish8<T>(P.f, c, m, n, left, v, bias, ws, r[p]);
+        for (int p = 0; p < 2; ++p) {
+          const int m = m0 + 32 * bi + 16 * p + (lane >> 2);
+          r[bi][p] = residual8<T>(P.f, c, m, n, m < P.M ? left : 0);
+        }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+#pragma unroll
+    for (int bi = 0; bi < Tile::TM / 32; ++bi) {
+      const int row = lane >> 2, m = m0 + 32 * bi + row;
+      // C of a 16 x 16 MFMA: lane l holds row l % 16, columns 4 (l / 16) .. + 3; of a
+      // 32 x 32 one: row l % 32, columns 8 q + 4 (l / 32) .. + 3, q = 0 .. 3
+      auto put = [&](int at, int x, f32x4 v) { *(lds_f32x4*)(mine + at * 128 + ((x ^ (at & 7)) << 4)) = v; };
+      if constexpr (Tile::MF == 16) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) put(16 * i + (lane & 15), 4 * j + (lane >> 4), acc[2 * bi + i][2 * bj + j]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          put(lane & 31, 2 * q + (lane >> 5),
+              f32x4{acc[bi][bj][4 * q], acc[bi][bj][4 * q + 1], acc[bi][bj][4 * q + 2], acc[bi][bj][4 * q + 3]});
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int at = row + 16 * p, x = 2 * (lane & 3);
+        const f32x4 lo = lds_get<f32x4>(mine + at * 128 + ((x ^ (at & 7)) << 4));
+        const f32x4 hi = lds_get<f32x4>(mine + at * 128 + (((x + 1) ^ (at & 7)) << 4));
+        const f32x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        if (m + 16 * p < P.M && left > 0) {
+          if (sums) store8(part + (int64_t)(m + 16 * p) * P.part_ld + n, 8, v);
+          else finish8<T>(P.f, c, m + 16 * p, n, left, v, bias, ws, r[bi][p]);
+        }
+      }
+      // the reads are issued before the next block's writes, and LDS runs a
+      // wave's accesses in order
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
   }
 }
 
@@ -582,6 +704,9 @@ inline lipz_mat launch_pack(const lipz_mat& m, void* dst, int rows, int cols, in
 
 // ---- the host's choices ----
 
+template <class E>
+constexpr bool kLarge = !std::is_same_v<E, float> && !std::is_same_v<E, Fp8>;
+
 enum { TILE_S = 0, TILE_M = 1, TILE_L = 2 };
 struct Plan {
   int tile, splits, per_split;
@@ -590,14 +715,15 @@ struct Plan {
 
 inline int tiles_of(int n, int b) { return (n + b - 1) / b; }
 
-inline Plan plan_gemm(int es, int M, int N, int K, int cells) {
+// large: whether there is a 256 x 256 kernel.
+inline Plan plan_gemm(int es, int M, int N, int K, int cells, bool large) {
   Plan p{TILE_S, 1, 0, 0};
   const int64_t l = (int64_t)tiles_of(M, 256) * tiles_of(N, 256) * cells, m = (int64_t)tiles_of(M, 128) * tiles_of(N, 128) * cells;
-  if (es < 4 && l >= 192) p.tile = TILE_L;
+  if (large && l >= 192) p.tile = TILE_L;
   else if (m >= 192) p.tile = TILE_M;
   const int b = p.tile == TILE_L ? 256 : p.tile == TILE_M ? 128 : 64;
   const int64_t tiles = (int64_t)tiles_of(M, b) * tiles_of(N, b) * cells;
-  const int slices = tiles_of(K * es, kSlice);
+  const int slices = tiles_of(K * es, p.tile == TILE_L ? 64 : 128);
   int splits = 1;
   if (p.tile == TILE_S && tiles < 256) {
     splits = (int)(512 / tiles);
@@ -623,8 +749,8 @@ inline void launch_gemm(GemmArgs& P, const Plan& plan, hipStream_t s) {
   if (plan.tile == ID) block_gemm_kernel<E, T, AKC, BKC, TILE><<<grid, TILE::NT, 0, s>>>(P);
   LIPZ_TILE(TILE_S, TileS)
   LIPZ_TILE(TILE_M, TileM)
-  if constexpr (ElemSize<E>::value < 4) {
-    LIPZ_TILE(TILE_L, TileL)
+  if constexpr (kLarge<E>) {
+    LIPZ_TILE(TILE_L, TileL<E>)
   }
 #undef LIPZ_TILE
   if (P.splits > 1) {
