@@ -425,8 +425,10 @@ typedef struct {
  * (the division by 448 is a product with its fp32 reciprocal, the other a
  * division);
  * a row that holds a NaN or an infinity then has the scale NaN and only NaN in
- * y.  residual, h and rstd may be NULL; h may be x or residual itself (same p,
- * ld and cell).  rows >= 0, 1 <= cols <= 2^20, eps > 0. */
+ * y.  A row whose squares' sum passes fp32's range has rstd 0.
+ * residual, h and rstd may be NULL; h may be x or residual itself (same p,
+ * ld and cell).  0 <= rows <= 2^30, 1 <= cols <= 2^20, eps > 0 (rows and cols
+ * also of the gradients). */
 typedef struct {
   int32_t abi_version, dtype, y_dtype, cells, rows, cols;
   float eps;

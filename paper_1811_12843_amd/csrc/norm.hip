@@ -20,6 +20,7 @@
 namespace lipz {
 namespace {
 
+constexpr int kMaxNormRows = 1 << 30;  // a row index and a grid's stride (2^16 at most) stay below 2^31
 
 struct NormArgs {
   const void *x, *r;
@@ -427,7 +428,7 @@ lipz_status check_norm(const lipz_rms_norm_args* a) {
   if (!a || a->abi_version != LIPZ_ABI_VERSION) return LIPZ_E_INVAL;
   if (!valid_float(a->dtype) || (a->y_dtype != a->dtype && a->y_dtype != LIPZ_FP8)) return LIPZ_E_INVAL;
   if (a->cells < 1 || a->rows < 0 || a->cols < 1 || !(a->eps > 0.f) || !(a->eps < __builtin_inff())) return LIPZ_E_INVAL;
-  if (a->cells > kMaxCells || a->cols > kMaxWide) return LIPZ_E_UNSUPPORTED;
+  if (a->cells > kMaxCells || a->rows > kMaxNormRows || a->cols > kMaxWide) return LIPZ_E_UNSUPPORTED;
   if (!a->x.p || !a->y.p || !a->gamma || (a->y_dtype == LIPZ_FP8 && !a->y_scale)) return LIPZ_E_INVAL;
   lipz_status st;
   if ((st = check_mat(a->x, a->cells, a->rows, a->cols, a->dtype, false))) return st;
@@ -442,7 +443,7 @@ lipz_status check_norm(const lipz_rms_norm_args* a) {
 lipz_status check_norm_bwd(const lipz_rms_norm_backward_args* a) {
   if (!a || a->abi_version != LIPZ_ABI_VERSION || !valid_float(a->dtype)) return LIPZ_E_INVAL;
   if (a->cells < 1 || a->rows < 0 || a->cols < 1) return LIPZ_E_INVAL;
-  if (a->cells > kMaxCells || a->cols > kMaxWide) return LIPZ_E_UNSUPPORTED;
+  if (a->cells > kMaxCells || a->rows > kMaxNormRows || a->cols > kMaxWide) return LIPZ_E_UNSUPPORTED;
   if (!a->h.p || !a->dy.p || !a->dx.p || !a->gamma || !a->rstd || (uintptr_t)a->rstd % 4) return LIPZ_E_INVAL;
   lipz_status st;
   if ((st = check_mat(a->h, a->cells, a->rows, a->cols, a->dtype, false))) return st;

@@ -147,3 +147,15 @@ def test_struct_layout_matches_c(name, tmp_path):
                                           check=True).stdout.split()]
     assert out[0] == ctypes.sizeof(cls)
     assert out[1:] == [getattr(cls, f).offset for f in fields]
+
+
+def test_norms_refuse_rows_whose_index_would_wrap():
+    for make, name in ((norm, "lipz_rms_norm"), (norm_bwd, "lipz_rms_norm_backward")):
+        far = {f: L.lipz_mat(P, 24, 24 << 31) for f, t in make()._fields_ if t is L.lipz_mat}
+        assert getattr(L, name + "_workspace_bytes")(make(rows=1 << 30, **far)) > 0
+        for rows in ((1 << 30) + 1, (1 << 31) - 1):
+            a = make(rows=rows, **far)
+            assert getattr(L, name + "_workspace_bytes")(a) == 0
+            with pytest.raises(L.LipzError) as e:
+                getattr(L, name)(a, P, 1 << 40, None)
+            assert e.value.status == L.LIPZ_E_UNSUPPORTED
