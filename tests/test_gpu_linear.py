@@ -340,3 +340,53 @@ def test_block_on_another_stream_and_in_a_graph():
         all_calls()
         torch.cuda.synchronize()
         assert torch.equal(y, got[0]) and torch.equal(z, got[1]), k
+
+
+# The largest tiles (two hundred and more of 256 x 256) with sums of many slices, odd ends on every side.
+WIDE = [(48, 300, 1032, 260), (48, 257, 2085, 511), (1, 3585, 1040, 3586)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("size", WIDE, ids=lambda s: "x".join(map(str, s)))
+def test_linear_on_the_largest_tiles(size, dtype):
+    C, M, K, N = size
+    dt, kind = TYPES[dtype][:2]
+    g = torch.Generator(device="cuda").manual_seed(K)
+    print(f"[case] largest tiles {dtype} {size}", flush=True)
+    x, w = padded(g, C, M, K, dt, 8), padded(g, C, K, N, dt, 6, K ** -0.5)
+    b, r = torch.randn(C, N, generator=g, device="cuda"), padded(g, C, M, N, dt, 2)
+    y, y_ok = blank(C, M, N, dt, 3)
+    pre, pre_ok = blank(C, M, N, dt)
+    forward(x, w, b, r, "gelu", pre, y)
+    z = torch.bmm(x.double(), w.double()) + b.double()[:, None]
+    t = off(x, w) + 2.0 ** -23 * z.abs()
+    want = act64("gelu", z) + r.double()
+    close(pre, z, dtype, t, "pre")
+    close(y, want, dtype, 1.2 * t + 1e-6 * (1 + z.abs()) + 2.0 ** -23 * want.abs(), "y")
+    assert y_ok() and pre_ok()
+    dx, dx_ok = blank(C, M, K, dt, 5)
+    dw, dw_ok = blank(C, K, N, dt, 5)
+    db = torch.empty(C, N, device="cuda")
+    backward(x, w, None, r, "linear", dx, dw, db)
+    wt, xt, dz = w.double().mT.contiguous(), x.double().mT.contiguous(), r.double()
+    close(dx, torch.bmm(dz, wt), dtype, off(dz, wt), "dx")
+    close(dw, torch.bmm(xt, dz), dtype, off(xt, dz), "dw")
+    close(db, dz.sum(1), "f32", 2.0 ** -23 * (16 + 2 * math.sqrt(M)) * dz.abs().sum(1), "db")
+    assert dx_ok() and dw_ok()
+
+
+@pytest.mark.parametrize("size", WIDE, ids=lambda s: "x".join(map(str, s)))
+def test_linear_fp8_on_the_largest_tiles(size):
+    C, M, K, N = size
+    g = torch.Generator(device="cuda").manual_seed(K + 1)
+    print(f"[case] largest tiles e4m3 {size}", flush=True)
+    x, w = padded(g, C, M, K, torch.float8_e4m3fn, 7, 50.0), padded(g, C, N, K, torch.float8_e4m3fn, 9, 50.0)
+    xs, ws = torch.rand(C, M, generator=g, device="cuda") * 0.02 + 0.01, torch.rand(C, N, generator=g, device="cuda") * 1e-3
+    y, y_ok = blank(C, M, N, torch.bfloat16, 3)
+    call("lipz_linear_fp8", L.lipz_linear_fp8_args(
+        y_dtype=L.LIPZ_BF16, cells=C, rows=M, fan_in=K, fan_out=N, act=CODE["silu"], slope=SLOPE, x=mat(x), w=mat(w),
+        y=mat(y), x_scale=xs.data_ptr(), x_scale_cell=M, w_scale=ws.data_ptr(), w_scale_cell=N))
+    wt, s = w.double().mT.contiguous(), xs.double()[:, :, None] * ws.double()[:, None]
+    z, t = torch.bmm(x.double(), wt) * s, off(x, wt) * s
+    close(y, act64("silu", z), "bf16", 1.2 * t + 1e-6 * (1 + z.abs()), "y")
+    assert y_ok()
