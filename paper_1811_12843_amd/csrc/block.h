@@ -73,6 +73,33 @@ template <class T>
 __device__ __forceinline__ f32x8 widen(typename Vec8<T>::type v) {
   return __builtin_convertvector(v, f32x8);
 }
+// Eight elements of a row from column col on (a multiple of 8) in two steps, so
+// that a row's end costs no branch before its loads: row8_raw loads the last
+// eight columns where fewer than eight are left (one at a time if the row has
+// fewer), and row8_in_place moves them to their places, zeros past the row.
+// One wide load where load8_raw takes up to seven that wait for each other.
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type row8_raw(const T* row, int col, int cols) {
+  if (cols < 8) return load8_raw(row + col, cols - col);
+  const LIPZ_GLOBAL T* p = (const LIPZ_GLOBAL T*)row + (col < cols - 8 ? col : cols - 8);
+  return reinterpret_cast<const LIPZ_GLOBAL Eight<T>*>(p)->v;
+}
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type row8_in_place(typename Vec8<T>::type v, int col, int cols) {
+  using Raw = typename Vec8<T>::type;
+  const int by = col - (cols - 8);
+  if (cols < 8 || by <= 0) return v;
+  if (by >= 8) return Raw{};
+  const Raw none = {};
+  if (by & 4) v = __builtin_shufflevector(v, none, 4, 5, 6, 7, 8, 8, 8, 8);
+  if (by & 2) v = __builtin_shufflevector(v, none, 2, 3, 4, 5, 6, 7, 8, 8);
+  if (by & 1) v = __builtin_shufflevector(v, none, 1, 2, 3, 4, 5, 6, 7, 8);
+  return v;
+}
+template <class T>
+__device__ __forceinline__ typename Vec8<T>::type row8(const T* row, int col, int cols) {
+  return row8_in_place<T>(row8_raw(row, col, cols), col, cols);
+}
 template <class T>
 __device__ __forceinline__ void store8(T* p, int n, f32x8 v) {
   const typename Vec8<T>::type w = __builtin_convertvector(v, typename Vec8<T>::type);

@@ -97,9 +97,10 @@ struct GemmArgs {
 constexpr uint32_t kPast = 0x80000000u;
 
 // ---- finishing: 8 columns of a row from column n on, `left` of them inside ----
+// (a residual as row8_raw loads it: finish8 puts it in place)
 template <class T>
-__device__ __forceinline__ typename Vec8<T>::type residual8(const Finish& f, int c, int m, int n, int left) {
-  return f.r ? load8_raw((const T*)f.r + c * f.r_cell + m * f.r_ld + n, left) : typename Vec8<T>::type{};
+__device__ __forceinline__ typename Vec8<T>::type residual8(const Finish& f, int c, int m, int n, int cols) {
+  return f.r ? row8_raw((const T*)f.r + c * f.r_cell + m * f.r_ld, n, cols) : typename Vec8<T>::type{};
 }
 template <class T>
 __device__ __forceinline__ void finish8(const Finish& f, int c, int m, int n, int left, f32x8 v, const f32x8& bias,
@@ -115,14 +116,14 @@ __device__ __forceinline__ void finish8(const Finish& f, int c, int m, int n, in
   if (f.pre) store8((T*)f.pre + c * f.pre_cell + m * f.pre_ld + n, left, v);
   v = act8<FAST>(f.act, v, f.slope);
   if (f.r) {
-    const f32x8 r = widen<T>(residual);
+    const f32x8 r = widen<T>(row8_in_place<T>(residual, n, n + left));
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += r[e];
   }
   store8((T*)f.y + c * f.y_cell + m * f.y_ld + n, left, v);
 }
-__device__ __forceinline__ f32x8 column8(const float* p, int64_t cell, int c, int n, int left) {
-  return p && left > 0 ? load8(p + c * cell + n, left) : f32x8{};
+__device__ __forceinline__ f32x8 column8(const float* p, int64_t cell, int c, int n, int cols) {
+  return p && n < cols ? row8(p + c * cell, n, cols) : f32x8{};
 }
 
 // ---- operands ----
@@ -557,8 +558,8 @@ __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) 
 #pragma unroll
   for (int bj = 0; bj < Tile::TN / 32; ++bj) {
     const int n = n0 + 32 * bj + 8 * (lane & 3), left = P.N - n;
-    const f32x8 bias = sums ? f32x8{} : column8(P.f.bias, P.f.bias_cell, c, n, left);
-    const f32x8 ws = sums ? f32x8{} : column8(P.f.ws, P.f.ws_cell, c, n, left);
+    const f32x8 bias = sums ? f32x8{} : column8(P.f.bias, P.f.bias_cell, c, n, P.N);
+    const f32x8 ws = sums ? f32x8{} : column8(P.f.ws, P.f.ws_cell, c, n, P.N);
     // all of the columns' residuals now: a load is waited for together with the stores before it
     typename Vec8<T>::type r[Tile::TM / 32][2] = {};
     if (P.f.r && !sums) {
@@ -566,8 +567,7 @@ __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) 
       for (int bi = 0; bi < Tile::TM / 32; ++bi)
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-          const int m = m0 + 32 * bi + 16 * p + (lane >> 2);
-          r[bi][p] = residual8<T>(P.f, c, m, n, m < P.M ? left : 0);
+          r[bi][p] = residual8<T>(P.f, c, min(m0 + 32 * bi + 16 * p + (lane >> 2), P.M - 1), n, P.N);
         }
     }
 #pragma unroll
@@ -619,15 +619,21 @@ __global__ __launch_bounds__(256) void join_splits_kernel(const GemmArgs P) {
   const int64_t row = at / per_row;
   const int n = 8 * (int)(at - row * per_row), c = (int)(row / P.M), m = (int)(row - (int64_t)c * P.M), left = P.N - n;
   const float* p = P.part + row * P.part_ld + n;
-  f32x8 v = load8(p, 8);
-  for (int s = 1; s < P.splits; ++s) {
-    p += rows * P.part_ld;
-    const f32x8 w = load8(p, 8);
+  f32x8 v = {};
+  // eight splits' sums in flight; past the last split the last one again, not added
+  for (int s0 = 0; s0 < P.splits; s0 += 8) {
+    f32x8 w[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
+    for (int u = 0; u < 8; ++u) w[u] = load8(p + min(s0 + u, P.splits - 1) * rows * P.part_ld, 8);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (s0 + u < P.splits) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += w[u][e];
+      }
   }
-  finish8<T>(P.f, c, m, n, left, v, column8(P.f.bias, P.f.bias_cell, c, n, left),
-             column8(P.f.ws, P.f.ws_cell, c, n, left), residual8<T>(P.f, c, m, n, left));
+  finish8<T>(P.f, c, m, n, left, v, column8(P.f.bias, P.f.bias_cell, c, n, P.N),
+             column8(P.f.ws, P.f.ws_cell, c, n, P.N), residual8<T>(P.f, c, m, n, P.N));
 }
 
 // ---- the host's checks, operands and workspaces ----

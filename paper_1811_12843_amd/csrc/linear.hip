@@ -36,16 +36,16 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs P) {
       Raw d[4], z[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int m = m0 + 8 * (i0 + i), in = m < P.M ? left : 0;
-        d[i] = load8_raw((const T*)P.dy + c * P.dy_cell + m * P.dy_ld + n, in);
-        z[i] = slopes ? load8_raw((const T*)P.pre + c * P.pre_cell + m * P.pre_ld + n, in) : Raw{};
+        const int m = min(m0 + 8 * (i0 + i), P.M - 1);
+        d[i] = row8_raw((const T*)P.dy + c * P.dy_cell + m * P.dy_ld, n, P.N);
+        z[i] = slopes ? row8_raw((const T*)P.pre + c * P.pre_cell + m * P.pre_ld, n, P.N) : Raw{};
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int m = m0 + 8 * (i0 + i);
-        f32x8 v = widen<T>(d[i]);
+        f32x8 v = widen<T>(row8_in_place<T>(d[i], n, P.N));
         if (slopes) {
-          const f32x8 w = slope8<(sizeof(T) < 4)>(P.act, widen<T>(z[i]), P.slope);
+          const f32x8 w = slope8<(sizeof(T) < 4)>(P.act, widen<T>(row8_in_place<T>(z[i], n, P.N)), P.slope);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= w[e];
           if (left < 8) {

@@ -40,11 +40,12 @@ __global__ __launch_bounds__(256) void column_max_kernel(const QuantArgs P) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int k = k0 + 8 * (i0 + i);
-        v[i] = load8_raw((const T*)P.w + c * P.w_cell + k * P.w_ld + n, k < P.K ? left : 0);
+        v[i] = row8_raw((const T*)P.w + c * P.w_cell + min(k, P.K - 1) * P.w_ld, n, P.N);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const f32x8 x = widen<T>(v[i]);
+        // (rows past the last one are that one again)
+        const f32x8 x = widen<T>(row8_in_place<T>(v[i], n, P.N));
 #pragma unroll
         for (int e = 0; e < 8; ++e) m[e] = max_nan(m[e], __builtin_fabsf(x[e]));
       }
@@ -72,12 +73,12 @@ __global__ __launch_bounds__(256) void quantize_kernel(const QuantArgs P) {
   __shared__ __attribute__((aligned(16))) T tile[kQuantRows][64];
   const int c = blockIdx.z, n0 = blockIdx.x * 64, k0 = blockIdx.y * kQuantRows, t = threadIdx.x;
   const int chunks = (P.K + kMaxRowsPer - 1) / kMaxRowsPer;
-  const int x = t & 7, left = P.N - n0 - 8 * x;
+  const int x = t & 7;
   Raw v[kQuantRows / 32];
 #pragma unroll
   for (int i = 0; i < kQuantRows / 32; ++i) {
     const int k = k0 + 32 * i + (t >> 3);
-    v[i] = load8_raw((const T*)P.w + c * P.w_cell + k * P.w_ld + n0 + 8 * x, k < P.K ? left : 0);
+    v[i] = row8_raw((const T*)P.w + c * P.w_cell + min(k, P.K - 1) * P.w_ld, n0 + 8 * x, P.N);
   }
   {
     const int col = t & 63, g = t >> 6;
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const QuantArgs P) {
 #pragma unroll
   for (int i = 0; i < kQuantRows / 32; ++i) {
     const int row = 32 * i + (t >> 3);
-    *(Raw*)&tile[row][8 * (x ^ ((row >> 3) & 7))] = v[i];
+    *(Raw*)&tile[row][8 * (x ^ ((row >> 3) & 7))] = row8_in_place<T>(v[i], n0 + 8 * x, P.N);
   }
   __syncthreads();
   if (t < 64) {

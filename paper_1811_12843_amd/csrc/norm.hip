@@ -104,17 +104,29 @@ __global__ __launch_bounds__(Group<TPR>::NT) void rms_norm_kernel(const NormArgs
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int col = 8 * (v * TPR + t);
-    gm[v] = col < P.cols ? load8(P.gamma + c * P.gamma_cell + col, P.cols - col) : f32x8{};
+    gm[v] = col < P.cols ? row8(P.gamma + c * P.gamma_cell, col, P.cols) : f32x8{};
   }
   for (int row = blockIdx.x * G::N + grp; row < P.rows; row += gridDim.x * G::N) {
     const T* x = (const T*)P.x + c * P.x_cell + row * P.x_ld;
     const T* r = P.r ? (const T*)P.r + c * P.r_cell + row * P.r_ld : nullptr;
     f32x8 h[NV];
+    typename Vec8<T>::type a[NV], b[NV];
     float ss = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int col = 8 * (v * TPR + t);
-      h[v] = col < P.cols ? residual_sum(x, r, col, P.cols) : f32x8{};
+      a[v] = col < P.cols ? row8_raw(x, col, P.cols) : typename Vec8<T>::type{};
+      if (r) b[v] = col < P.cols ? row8_raw(r, col, P.cols) : typename Vec8<T>::type{};
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int col = 8 * (v * TPR + t);
+      h[v] = widen<T>(row8_in_place<T>(a[v], col, P.cols));
+      if (r) {
+        const f32x8 w = widen<T>(row8_in_place<T>(b[v], col, P.cols));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[v][e] += w[e];
+      }
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -208,7 +220,7 @@ __global__ __launch_bounds__(Group<TPR>::NT) void rms_norm_bwd_kernel(const Norm
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int col = 8 * (v * TPR + t);
-    gm[v] = col < P.cols ? load8(P.gamma + c * P.gamma_cell + col, P.cols - col) : f32x8{};
+    gm[v] = col < P.cols ? row8(P.gamma + c * P.gamma_cell, col, P.cols) : f32x8{};
     dg[v] = f32x8{};
   }
   for (int row = blockIdx.x * G::N + grp; row < P.rows; row += gridDim.x * G::N) {
@@ -220,13 +232,17 @@ __global__ __launch_bounds__(Group<TPR>::NT) void rms_norm_bwd_kernel(const Norm
     float s = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int col = 8 * (v * TPR + t), n = P.cols - col;
-      h[v] = n > 0 ? load8_raw(hp + col, n) : typename Vec8<T>::type{};
-      dy[v] = n > 0 ? load8_raw(yp + col, n) : typename Vec8<T>::type{};
-      dh[v] = n > 0 && rp ? load8_raw(rp + col, n) : typename Vec8<T>::type{};
+      const int col = 8 * (v * TPR + t);
+      h[v] = col < P.cols ? row8_raw(hp, col, P.cols) : typename Vec8<T>::type{};
+      dy[v] = col < P.cols ? row8_raw(yp, col, P.cols) : typename Vec8<T>::type{};
+      dh[v] = col < P.cols && rp ? row8_raw(rp, col, P.cols) : typename Vec8<T>::type{};
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+      const int col = 8 * (v * TPR + t);
+      h[v] = row8_in_place<T>(h[v], col, P.cols);
+      dy[v] = row8_in_place<T>(dy[v], col, P.cols);
+      dh[v] = row8_in_place<T>(dh[v], col, P.cols);
       const f32x8 x = widen<T>(h[v]), d = widen<T>(dy[v]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
