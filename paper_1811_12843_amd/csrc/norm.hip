@@ -14,7 +14,9 @@
 // pass, which keeps more of a row) are read again for each of their passes
 // instead.
 //
-// Bound by memory.
+// Bound by memory, each input read once: 16384 x 4096 bf16 with residual 105 us
+// (5.1 TB/s; a large copy runs at 4.8), gradients of 8192 x 8192 bf16 107 us (5.0
+// TB/s, 6 us of it the columns' sums); one row of 4096 to e4m3 6.6 us, a launch.
 #include "block.h"
 
 namespace lipz {
