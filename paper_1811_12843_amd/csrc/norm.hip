@@ -14,15 +14,15 @@
 // pass, which keeps more of a row) are read again for each of their passes
 // instead.
 //
-// Bound by memory, each input read once: 16384 x 4096 bf16 with residual 105 us
-// (5.1 TB/s; a large copy runs at 4.8), gradients of 8192 x 8192 bf16 107 us (5.0
+// Bound by memory, each input read once: 16384 x 4096 bf16 with residual 94 us
+// (5.7 TB/s; a large copy runs at 4.8), gradients of 8192 x 8192 bf16 107 us (5.0
 // TB/s, 6 us of it the columns' sums); one row of 4096 to e4m3 6.6 us, a launch.
 #include "block.h"
 
 namespace lipz {
 namespace {
 
-constexpr int kMaxNormRows = 1 << 30;  // a row index and a grid's stride (2^16 at most) stay below 2^31
+constexpr int kMaxNormRows = 1 << 30;  // a row index and a grid's stride (2^17 at most) stay below 2^31
 
 struct NormArgs {
   const void *x, *r;
@@ -391,15 +391,19 @@ void row_shape(int cols, int most, int& tpr, int& nv) {
 }
 int groups_of(int tpr) { return tpr && tpr < 256 ? 256 / tpr : 1; }
 
-// Blocks per cell: enough of them to fill the card's 256 compute units with
-// 2048 threads each, no more than there are rows for.
+// Blocks per cell, of `most` over all cells, no more than there are rows for.
+// Forward, a row per block up to 16384 blocks for rows over 2048 columns:
+// rows then start as others end (16384 x 4096 bf16 94 us; 4096 blocks 99, 2048
+// 105); 4096 for shorter ones, which share a block (200000 x 64 bf16 19.1 us;
+// 16384 blocks 20.6, 2048 19.6); 512 for blocks of 1024 threads, two to a compute
+// unit (2048 x 32768 bf16 108 us, 2048 blocks 115).  Backward 512: each adds a row
+// to the columns' partial sums.
 int norm_blocks(int rows, int cells, int tpr, int most) {
   const int per = groups_of(tpr);
-  const int want = (most + cells - 1) / cells;
-  const int have = (rows + per - 1) / per;
+  const int want = (most + cells - 1) / cells, have = (rows + per - 1) / per;
   return have < want ? have : want;
 }
-int fwd_blocks(int rows, int cells, int tpr) { return norm_blocks(rows, cells, tpr, tpr == 0 || tpr == 1024 ? 512 : 2048); }
+int fwd_blocks(int rows, int cells, int tpr) { return norm_blocks(rows, cells, tpr, tpr == 0 || tpr == 1024 ? 512 : tpr == 256 ? 16384 : 4096); }
 int bwd_blocks(int rows, int cells, int tpr) { return norm_blocks(rows, cells, tpr, 512); }
 
 template <class F>
