@@ -244,7 +244,7 @@ __device__ __forceinline__ float wave_max_nan(float v) {
 
 constexpr int64_t kMaxWide = 1 << 20;  // columns of a matrix
 constexpr int kMaxCells = 65535;       // a grid's second dimension
-constexpr int kMaxRows = 1 << 21;      // rows of a product, in blocks of 64 a grid's second dimension
+constexpr int kMaxRows = 1 << 21;      // rows of a product
 
 inline int elem_size(int dtype) { return dtype == LIPZ_F32 ? 4 : dtype == LIPZ_FP8 ? 1 : 2; }
 inline bool valid_float(int dtype) { return dtype == LIPZ_F32 || dtype == LIPZ_BF16 || dtype == LIPZ_F16; }

@@ -3,21 +3,23 @@
 //
 // Backward: one pass forms dz = dy act'(pre), rounds it to the operands' type
 // for the two products (which take it from L2 or the Infinity Cache), and
-// sums its columns, unrounded, per 64 rows; a second adds those for db.  dx =
+// sums its columns, unrounded, per 32 rows; a second adds those for db.  dx =
 // dz w^T reads both operands along k; dw = x^T dz both across it.
-// At 8192 x 4096 x 4096 bf16, 504 us together: dz 48 us (201 MB, 4.2 TB/s), the
-// products 246 and 216 us (1.1 and 1.3 PFLOP/s).
+// At 8192 x 4096 x 4096 bf16, 488 us together: dz 35 to 42 us (201 MB, 4.8 TB/s and
+// more), the products 244 and 212 us (1.1 and 1.3 PFLOP/s).
 #include "block_gemm.h"
 
 namespace lipz {
 namespace {
 
-constexpr int kRowsPer = 64;  // rows of dz that a block sums
+// Rows of dz that a block sums.  32 rather than 64: 1999 x 777 f16 7 us instead
+// of 13.  (Blocks of a cell: under 2^24, by check_tiles.)
+constexpr int kRowsPer = 32;
 
 struct SlopeArgs {
   const void *dy, *pre;
   void* dz;     // [..][dz_ld], zeros past N; NULL: only the sums
-  float* part;  // [cells][ceil(M / 64)][N], NULL without db
+  float* part;  // [cells][ceil(M / 32)][N], NULL without db
   int64_t dy_ld, dy_cell, pre_ld, pre_cell, dz_ld, dz_cell;
   int M, N, act;
   float slope;
@@ -28,8 +30,9 @@ template <class T>
 __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs P) {
   using Raw = typename Vec8<T>::type;
   __shared__ float sums[8][256 + 8];
-  const int c = blockIdx.z, lane = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int n = blockIdx.x * 256 + 8 * lane, left = P.N - n, m0 = blockIdx.y * kRowsPer + r;
+  const int c = blockIdx.y, lane = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int wide = (P.N + 255) / 256, chunk = blockIdx.x / wide, n0 = (blockIdx.x - chunk * wide) * 256;
+  const int n = n0 + 8 * lane, left = P.N - n, m0 = chunk * kRowsPer + r;
   const bool slopes = P.act != LIPZ_ACT_LINEAR;
   f32x8 s = {};
   if (left > 0 || (P.dz && n < P.dz_ld)) {
@@ -67,12 +70,12 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs P) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) sums[r][8 * lane + e] = s[e];
   __syncthreads();
-  const int col = blockIdx.x * 256 + threadIdx.x;
+  const int col = n0 + threadIdx.x;
   if (col >= P.N) return;
   float t = 0.f;
 #pragma unroll
   for (int q = 0; q < 8; ++q) t += sums[q][threadIdx.x];
-  P.part[((int64_t)c * gridDim.y + blockIdx.y) * P.N + col] = t;
+  P.part[((int64_t)c * (gridDim.x / wide) + chunk) * P.N + col] = t;
 }
 
 lipz_status check_linear(const lipz_linear_args* a) {
@@ -212,7 +215,7 @@ lipz_status run_linear_bwd(const lipz_linear_backward_args* a, void* ws, hipStre
     S.dz = w.copy_dz ? dz.p : nullptr, S.dz_ld = dz.ld, S.dz_cell = dz.cell;
     S.part = a->db ? (float*)(base + w.part) : nullptr;
     S.M = M, S.N = N, S.act = a->act, S.slope = a->slope;
-    slope_kernel<T><<<dim3(tiles_of(N, 256), w.chunks, C), 256, 0, s>>>(S);
+    slope_kernel<T><<<dim3(w.chunks * tiles_of(N, 256), C), 256, 0, s>>>(S);
     if (a->db && launch_sum_parts(S.part, w.chunks, N, C, a->db, a->db_cell, s) != hipSuccess) return LIPZ_E_HIP;
   }
   if (a->dx.p) {
