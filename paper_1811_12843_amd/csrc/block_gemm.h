@@ -14,8 +14,7 @@
 // NS on.  Tiles of 64 and 128 rows: SB = 128 (32 k of fp32, 64 of 16 bits, 128 of
 // e4m3); of 256 rows: SB = 64.  MFMAs are 16 x 16 (one 16 x 16 x 32 moves less
 // between registers than a 32 x 32 x 16, and the card's power is what bounds
-// large products: 8192 x 4096 x 4096 bf16 along k 212 and 229 us), for e4m3 on
-// large tiles 32 x 32 x 64.
+// large products: 8192 x 4096 x 4096 bf16 along k 212 and 229 us).
 //
 // LDS.  KC: a row of 128 bytes is eight 16-byte chunks, chunk c at place
 // c ^ (row % 8) (of 64 bytes four, at c ^ (-(row / 4) % 4)): a 16-byte read serves
@@ -38,10 +37,8 @@
 // card's power leaves and by the finish, whose memory traffic overlaps no other
 // tile's products (the stages take 128 KiB of LDS, so a compute unit holds one
 // workgroup): 8192 x 4096 x 8192 bf16 with GELU, residual and pre 525 us (1.05
-// PFLOP/s, matrix cores 49 % busy), e4m3 8192 x 8192 x 4096 264 us (2.1 PFLOP/s).
-// The finish as a loop over the wave's columns takes 563 us of the former.
-// Four waves of 128 x 128 instead of eight for e4m3, with that loop (without it
-// the sums spill): 324 us instead of 306, both with the weights' quantisation.
+// PFLOP/s, matrix cores 49 % busy); with the finish as a loop over the wave's
+// columns 563 us.  e4m3 8192 x 8192 x 4096 with the weights' quantisation 590 us.
 // One row: the weights' bytes, 4096 x 4096 bf16 12.3 us, 7 of them the product.
 #pragma once
 
@@ -49,18 +46,18 @@
 
 namespace lipz {
 
-// The operand types of e4m3 products, by how they are formed.  The e4m3 MFMAs
-// (16 x 16 x 32 and, at twice the rate, 16 x 16 x 128) align their products to the
-// largest before they add them: measured on normal operands, both give sums that
-// are 1.4e-5 off in the 2-norm, at most 1.2e-5 (K = 128), 3.2e-6 (1024), 1.0e-6
-// (8192) of the sum of magnitudes.  Fp8Wide takes the second.  Fp8 turns the
-// fragments into f16, which holds every e4m3 value, and multiplies at fp32 accuracy.
+// The operand type of e4m3 products.  Their fragments are turned into f16, which
+// holds every e4m3 value, and multiplied at fp32 accuracy.  The e4m3 MFMAs, at up to
+// twice the rate, align their products to the largest of their k before they add
+// them, so that one large product takes the low bits of all others: sums of 1024
+// with a 448 x 448 of either sign in every 64 terms and remainders between 1 and 4
+// came out up to 8.7e-5 of the sum of magnitudes and 12 % of their value off (in f16:
+// below 1e-7 and 2.4e-4).  That costs 590 us instead of 307 at 8192 x 8192 x 4096, and
+// 13.0 instead of 11.7 at 8 x 4096 x 8192.
 struct Fp8 {};
-struct Fp8Wide {};
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_any;
 typedef __attribute__((address_space(3))) char lds_char;
@@ -77,10 +74,6 @@ struct ElemSize {
 };
 template <>
 struct ElemSize<Fp8> {
-  static constexpr int value = 1;
-};
-template <>
-struct ElemSize<Fp8Wide> {
   static constexpr int value = 1;
 };
 
@@ -261,8 +254,8 @@ struct Fragments<2, false, R, 16, SB, N> {
   }
 };
 
-// For 32 x 32 MFMAs, slices of 64 bytes: lane l holds row l % 32; 16 bits: k = 16 kk +
-// 8 (l / 32) .. + 7; e4m3 (whole slices): chunks l / 32 and 2 + l / 32.
+// For 32 x 32 MFMAs, slices of 64 bytes: lane l holds row l % 32, k = 16 kk +
+// 8 (l / 32) .. + 7 (16 bits).
 template <int ES, int R, int N>
 struct Fragments<ES, true, R, 32, 64, N> {
   static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
@@ -333,8 +326,7 @@ struct TileShape {
 // instead of 43.4)
 typedef TileShape<64, 64, 2, 2, 3, 128, 16> TileS;
 typedef TileShape<128, 128, 2, 2, 4, 128, 16> TileM;
-template <class E>
-using TileL = TileShape<256, 256, 2, 4, 4, 64, std::is_same_v<E, Fp8Wide> ? 32 : 16>;
+typedef TileShape<256, 256, 2, 4, 4, 64, 16> TileL;
 
 // Waits until all but this wave's last n vector loads have landed and its LDS
 // accesses are done, then for the other waves.  No more than that: the
@@ -394,8 +386,8 @@ struct Parts<E, AKC, BKC, Tile, false> {
 };
 
 // e4m3: a part is half of the wave's rows.
-template <bool WIDE, class Tile>
-struct Fp8Parts {
+template <bool AKC, bool BKC, class Tile>
+struct Parts<Fp8, AKC, BKC, Tile, false> {
   static constexpr int H = Tile::MI / 2;
   u32x4 fb[2][2][Tile::NI], fa[2][2][H];  // B's serve both parts: fb[1] are the ones of the part that is left
   __device__ __forceinline__ void turn() {
@@ -416,36 +408,19 @@ struct Fp8Parts {
   __device__ __forceinline__ void mma(typename Tile::Acc (&acc)[Tile::MI][Tile::NI]) {
     const auto& a = fa[P];
     const auto& b = fb[P];
-    if constexpr (WIDE) {
 #pragma unroll
-      for (int i = 0; i < H; ++i)
+    for (int q = 0; q < 4; ++q) {
+      f16x8 w[Tile::NI];
 #pragma unroll
-        for (int j = 0; j < Tile::NI; ++j) {
-          // operand formats 0: e4m3; block scales 2^0
-          const i32x8 w = join(b[0][j], b[1][j]), x = join(a[0][i], a[1][i]);
-          if constexpr (Tile::MF == 16)
-            acc[H * P + i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[H * P + i][j], 0, 0, 0, 127, 0, 127);
-          else
-            acc[H * P + i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc[H * P + i][j], 0, 0, 0, 127, 0, 127);
-        }
-    } else {
+      for (int j = 0; j < Tile::NI; ++j) w[j] = eight(b[q / 2][j], q);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f16x8 w[Tile::NI];
+      for (int i = 0; i < H; ++i) {
+        const f16x8 x = eight(a[q / 2][i], q);
 #pragma unroll
-        for (int j = 0; j < Tile::NI; ++j) w[j] = eight(b[q / 2][j], q);
-#pragma unroll
-        for (int i = 0; i < H; ++i) {
-          const f16x8 x = eight(a[q / 2][i], q);
-#pragma unroll
-          for (int j = 0; j < Tile::NI; ++j)
-            acc[H * P + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[j], x, acc[H * P + i][j], 0, 0, 0);
-        }
+        for (int j = 0; j < Tile::NI; ++j)
+          acc[H * P + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[j], x, acc[H * P + i][j], 0, 0, 0);
       }
     }
-  }
-  static __device__ __forceinline__ i32x8 join(u32x4 lo, u32x4 hi) {
-    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   }
   // bytes 8 (q % 2) .. + 7 of a fragment
   static __device__ __forceinline__ f16x8 eight(u32x4 v, int q) {
@@ -461,10 +436,6 @@ struct Fp8Parts {
     return r;
   }
 };
-template <bool AKC, bool BKC, class Tile>
-struct Parts<Fp8, AKC, BKC, Tile, false> : Fp8Parts<false, Tile> {};
-template <bool AKC, bool BKC, class Tile>
-struct Parts<Fp8Wide, AKC, BKC, Tile, false> : Fp8Parts<true, Tile> {};
 
 // The tile of a workgroup.  Workgroup b runs on XCD b % 8: each XCD takes a
 // contiguous share of the tiles, and tiles follow each other down `GM` rows
@@ -769,7 +740,7 @@ inline void launch_gemm(GemmArgs& P, const Plan& plan, hipStream_t s) {
   LIPZ_TILE(TILE_S, TileS)
   LIPZ_TILE(TILE_M, TileM)
   if constexpr (kLarge<E>) {
-    LIPZ_TILE(TILE_L, TileL<E>)
+    LIPZ_TILE(TILE_L, TileL)
   }
 #undef LIPZ_TILE
   if (P.splits > 1) {

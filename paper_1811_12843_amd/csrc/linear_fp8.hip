@@ -13,10 +13,6 @@
 namespace lipz {
 namespace {
 
-// Sums at least this long, for 16-bit outputs, are formed by the wide MFMA: its
-// error is then below the bound on fp32's own rounding of such a sum, and a
-// hundredth of the output's rounding.
-constexpr int kWideMin = 1024;
 constexpr int kMaxRowsPer = 256;  // rows of w whose maxima one block takes
 
 struct QuantArgs {
@@ -151,8 +147,6 @@ void run_quant(const QuantArgs& P, int cells, hipStream_t s) {
   quantize_kernel<T><<<dim3(tiles_of(P.N, 64), tiles_of(P.K, kQuantRows), cells), 256, 0, s>>>(P);
 }
 
-bool wide_sums(const lipz_linear_fp8_args* a) { return elem_size(a->y_dtype) == 2 && a->fan_in >= kWideMin; }
-
 struct Fp8Layout {
   bool pack_x = false, pack_w = false;
   size_t x = 0, w = 0, sums = 0, total = 256;
@@ -167,7 +161,7 @@ Fp8Layout fp8_layout(const lipz_linear_fp8_args* a) {
   w.pack_w = !loads_as_is(a->w, K, 1, true);
   if (w.pack_x) w.x = b.take(packed_bytes(M, K, 1, C));
   if (w.pack_w) w.w = b.take(packed_bytes(N, K, 1, C));
-  w.plan = plan_gemm(1, M, N, K, C, wide_sums(a));
+  w.plan = plan_gemm(1, M, N, K, C, false);
   w.sums = b.take(w.plan.part_bytes);
   w.total = b.at + 256;
   return w;
@@ -187,9 +181,6 @@ void run_linear_fp8(const lipz_linear_fp8_args* a, void* ws, hipStream_t s) {
   f.r = a->residual.p, f.r_ld = a->residual.ld, f.r_cell = a->residual.cell;
   f.bias = a->bias, f.bias_cell = a->bias_cell, f.act = a->act, f.slope = a->slope;
   f.xs = a->x_scale, f.xs_cell = a->x_scale_cell, f.ws = a->w_scale, f.ws_cell = a->w_scale_cell;
-  if constexpr (sizeof(T) == 2) {
-    if (wide_sums(a)) return launch_gemm<Fp8Wide, T, true, true>(P, w.plan, s);
-  }
   launch_gemm<Fp8, T, true, true>(P, w.plan, s);
 }
 

@@ -1,0 +1,55 @@
+"""Accuracy of the residual-block operators where values of very different sizes meet, against the formulas in 64 bits.
+
+Tolerances.  Sums: 2^-23 (16 + 2 sqrt(n)) sum |p| for n products p, as for sums in fp32 of any operands, and half a unit
+in the last place of the output's type."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import paper_1811_12843_amd as L  # noqa: E402
+
+from block_harness import TYPES, blank, call, close, mat  # noqa: E402
+
+F8 = torch.float8_e4m3fn
+
+
+def outliers(kind, rows, K, g):
+    """Rows of e4m3 values whose products with each other are led by a few: small ones of one sign, and 448 in places.
+    one: a single place; groups: every 64th; signs: every 64th, one row's set in turn plus and minus."""
+    v = 1 + torch.rand(2, rows, K, generator=g, device="cuda")
+    if kind == "one":
+        v[:, :, K // 3] = 448
+    else:
+        v[:, :, 5::64] = 448
+    if kind == "signs":
+        v[1, :, 5::128] = -448
+    return v.to(F8)
+
+
+@pytest.mark.parametrize("kind", ["one", "groups", "signs"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+# on 64 x 64 tiles, with the sum split and whole; and on larger ones
+@pytest.mark.parametrize("size", [(3, 1024, 70), (70, 8192, 136), (1030, 1040, 1100), (1800, 1101, 1700)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_e4m3_sums_with_outliers(size, dtype, kind):
+    """The small products count as much as they do in an fp32 sum: x [M][K] of one row kind times w [N][K]."""
+    M, K, N = size
+    dt, code = TYPES[dtype][:2]
+    g = torch.Generator(device="cuda").manual_seed(K + N)
+    print(f"[case] e4m3 outliers {dtype} {size} {kind}", flush=True)
+    both = outliers(kind, max(M, N), K, g)
+    x, w = both[:1, :M].contiguous(), both[1:, :N].contiguous()
+    # powers of two that keep every output in f16's range
+    xs = torch.full((1, M), 2.0 ** -8, device="cuda")
+    ws = torch.full((1, N), 2.0 ** -14, device="cuda")
+    y, ok = blank(1, M, N, dt, 3)
+    call("lipz_linear_fp8", L.lipz_linear_fp8_args(
+        y_dtype=code, cells=1, rows=M, fan_in=K, fan_out=N, x=mat(x), w=mat(w), y=mat(y), x_scale=xs.data_ptr(),
+        x_scale_cell=M, w_scale=ws.data_ptr(), w_scale_cell=N))
+    wt = w.double().mT.contiguous()
+    z, size1 = torch.bmm(x.double(), wt), torch.bmm(x.double().abs(), wt.abs())
+    close(y, z * 2.0 ** -22, dtype, 2.0 ** -23 * (16 + 2 * math.sqrt(K)) * size1 * 2.0 ** -22, "y")
+    assert ok()
