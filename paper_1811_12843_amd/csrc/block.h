@@ -149,9 +149,11 @@ __device__ __forceinline__ float fp8_scale(float m) {
 }
 
 // ---- activations: z -> act(z), and act'(z) ----
-// FAST: for outputs that are rounded to 16 bits.  erf by Abramowitz and
-// Stegun 7.1.26 (absolute error 1.5e-7), exponentials and reciprocals of the
-// hardware's 1 ulp; else the library's functions.
+// FAST: for outputs that are rounded to 16 bits.  erfc as below, exponentials and
+// reciprocals of the hardware's 1 ulp; else the library's functions.  Neither takes
+// a small value as the difference of large ones: GELU and the slopes keep their
+// relative accuracy down to the smallest normal numbers (but for e^(-z^2 / 2)'s own
+// z^2 2^-23, and where a slope passes through 0).
 
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 
@@ -166,13 +168,18 @@ __device__ __forceinline__ float recip(float x) {
 // Phi(z); with FAST e must be e^(-z^2 / 2)
 template <bool FAST>
 __device__ __forceinline__ float normal_cdf(float z, float e) {
-  if (!FAST) return 0.5f * (1.f + erff(z * kInvSqrt2));
+  if (!FAST) return 0.5f * erfcf(-z * kInvSqrt2);
+  // erfc(x) e^(x^2), 0 <= x <= 12, as a polynomial of t = 1 / (1 + 0.376 x) without a
+  // constant term: a least-squares fit of the ratio, weighted until its largest
+  // errors are alike, 8.3e-7 (of Phi(-|z|) itself, wherever z lies)
   const float x = __builtin_fabsf(z) * kInvSqrt2;
-  const float t = recip<true>(fmaf(0.3275911f, x, 1.f));
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f);
+  const float t = recip<true>(fmaf(0.376f, x, 1.f));
+  float p = fmaf(-0.13225922f, t, 0.37415940f);
+  p = fmaf(p, t, -0.11272450f);
+  p = fmaf(p, t, 0.27244622f);
+  p = fmaf(p, t, 0.17082962f);
+  p = fmaf(p, t, 0.21559894f);
+  p = fmaf(p, t, 0.21194951f);
   const float q = 0.5f * p * t * e;  // Phi(-|z|)
   return z < 0.f ? q : 1.f - q;
 }
@@ -210,9 +217,9 @@ __device__ __forceinline__ f32x8 slope8(int act, f32x8 z, float slope) {
     case LIPZ_ACT_RELU: return each8(z, [](float v) { return v > 0.f ? 1.f : (v <= 0.f ? 0.f : v); });
     case LIPZ_ACT_LRELU: return each8(z, [=](float v) { return v > 0.f ? 1.f : (v <= 0.f ? slope : v); });
     case LIPZ_ACT_TANH:
-      return each8(z, [](float v) {
-        const float t = tanh_of<FAST>(v);
-        return fmaf(-t, t, 1.f);
+      return each8(z, [](float v) {  // 1 - tanh^2
+        const float e = exp_of<FAST>(-2.f * __builtin_fabsf(v)), q = recip<FAST>(1.f + e);
+        return 4.f * e * q * q;
       });
     case LIPZ_ACT_GELU:
       return each8(z, [](float v) {

@@ -53,3 +53,55 @@ def test_e4m3_sums_with_outliers(size, dtype, kind):
     z, size1 = torch.bmm(x.double(), wt), torch.bmm(x.double().abs(), wt.abs())
     close(y, z * 2.0 ** -22, dtype, 2.0 ** -23 * (16 + 2 * math.sqrt(K)) * size1 * 2.0 ** -22, "y")
     assert ok()
+
+
+CODE = dict(L.ACTS, gelu=L.LIPZ_ACT_GELU, silu=L.LIPZ_ACT_SILU)
+SLOPE = 0.2
+
+
+def act_and_slope(name, z):
+    """act(z), act'(z) and the sums of the magnitudes of the terms that they are, on the CPU (z in 64 bits)."""
+    if name == "gelu":
+        cdf = 0.5 * torch.special.erfc(-z / math.sqrt(2))
+        d = z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+        return z * cdf, cdf + d, (z * cdf).abs(), cdf + d.abs()
+    if name == "silu":
+        s, c = 1 / (1 + torch.exp(-z)), 1 / (1 + torch.exp(z))
+        return z * s, s * (1 + z * c), (z * s).abs(), s * (1 + (z * c).abs())
+    e = torch.exp(-2 * z.abs())
+    d = 4 * e / (1 + e) ** 2
+    return torch.tanh(z), d, torch.tanh(z).abs(), d
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("act", ["gelu", "silu", "tanh"])
+def test_activations_and_slopes_keep_their_tails(act, dtype):
+    """act(z) by a bias alone and act'(z) by a gradient of ones, z from -12 to 12.
+
+    Tolerance, relative to the terms' sum: 2^-23 (16 + 2 z^2), a few roundings and functions of 1 or 2 units each, and
+    for an exponential or erfc that of an argument near z^2 / 2 or 2 |z|; 16-bit types' own approximations 2e-6 more,
+    far below their rounding."""
+    dt, code = TYPES[dtype][:2]
+    z = torch.arange(-12 * 64, 12 * 64 + 1, device="cuda") / 64.0
+    N = z.numel()
+    x, w = torch.zeros(1, 1, 1, device="cuda", dtype=dt), torch.ones(1, 1, N, device="cuda", dtype=dt)
+    y, ok = blank(1, 1, N, dt, 3)
+    call("lipz_linear", L.lipz_linear_args(
+        dtype=code, cells=1, rows=1, fan_in=1, fan_out=N, act=CODE[act], slope=SLOPE, x=mat(x), w=mat(w), y=mat(y),
+        bias=z.data_ptr(), bias_cell=N))
+    own = 0.0 if dtype == "f32" else 2e-6
+
+    def tol(z, terms):
+        return (2.0 ** -23 * (16 + 2 * z * z) + own) * terms
+
+    zd = z.double().cpu()
+    a, _, terms, _ = act_and_slope(act, zd)
+    close(y[0, 0], a, dtype, tol(zd, terms), "act")
+    assert ok()
+    pre, dy, db = z.to(dt).view(1, 1, N), torch.ones(1, 1, N, device="cuda", dtype=dt), torch.empty(1, N, device="cuda")
+    call("lipz_linear_backward", L.lipz_linear_backward_args(
+        dtype=code, cells=1, rows=1, fan_in=1, fan_out=N, act=CODE[act], slope=SLOPE, pre=mat(pre), dy=mat(dy),
+        db=db.data_ptr(), db_cell=N))
+    zd = pre[0, 0].double().cpu()
+    _, d, _, terms = act_and_slope(act, zd)
+    close(db[0], d, "f32", tol(zd, terms), "slope")
