@@ -407,7 +407,8 @@ lipz_status lipz_gemm_timing(lipz_grid* g, double* h_ms, int64_t* h_launches, do
  * call) before anything is enqueued, LIPZ_E_HIP. */
 enum { LIPZ_F32 = 0, LIPZ_BF16 = 1, LIPZ_F16 = 2, LIPZ_FP8 = 3 };
 /* Activations of these operators, beside LIPZ_ACT_LINEAR .. LIPZ_ACT_TANH:
- * GELU z Phi(z) (Phi the normal distribution function), SiLU z / (1 + e^-z). */
+ * GELU z Phi(z) (Phi the normal distribution function), SiLU z / (1 + e^-z).
+ * At infinite z activations and slopes are their limits. */
 enum { LIPZ_ACT_GELU = 4, LIPZ_ACT_SILU = 5 };
 #define LIPZ_MAX_LD ((int64_t)1 << 20)
 

@@ -192,6 +192,13 @@ __device__ __forceinline__ float tanh_of(float z) {
   return z2 < 0.0625f ? small : big;
 }
 
+// GELU, SiLU and their slopes at infinite z are their limits, not 0 times infinity: z
+// goes no lower than where e^z and Phi(z) are 0 in fp32, and for the slopes no
+// higher than where their complements are.  (A comparison keeps a NaN.)
+constexpr float kFarOut = 128.f;
+__device__ __forceinline__ float not_below(float z) { return z < -kFarOut ? -kFarOut : z; }
+__device__ __forceinline__ float inside(float z) { return z > kFarOut ? kFarOut : not_below(z); }
+
 // Eight at a time: one branch on the activation for all of them.
 template <class F>
 __device__ __forceinline__ f32x8 each8(f32x8 z, F f) {
@@ -206,8 +213,15 @@ __device__ __forceinline__ f32x8 act8(int act, f32x8 z, float slope) {
     case LIPZ_ACT_LRELU: return each8(z, [=](float v) { return v < 0.f ? slope * v : v; });
     case LIPZ_ACT_TANH: return each8(z, [](float v) { return tanh_of<FAST>(v); });
     case LIPZ_ACT_GELU:
-      return each8(z, [](float v) { return v * normal_cdf<FAST>(v, FAST ? exp_of<true>(-0.5f * v * v) : 0.f); });
-    case LIPZ_ACT_SILU: return each8(z, [](float v) { return v * recip<FAST>(1.f + exp_of<FAST>(-v)); });
+      return each8(z, [](float v) {
+        v = not_below(v);
+        return v * normal_cdf<FAST>(v, FAST ? exp_of<true>(-0.5f * v * v) : 0.f);
+      });
+    case LIPZ_ACT_SILU:
+      return each8(z, [](float v) {
+        v = not_below(v);
+        return v * recip<FAST>(1.f + exp_of<FAST>(-v));
+      });
     default: return z;
   }
 }
@@ -223,11 +237,13 @@ __device__ __forceinline__ f32x8 slope8(int act, f32x8 z, float slope) {
       });
     case LIPZ_ACT_GELU:
       return each8(z, [](float v) {
+        v = inside(v);
         const float e = exp_of<FAST>(-0.5f * v * v);
         return fmaf(v * kInvSqrt2Pi, e, normal_cdf<FAST>(v, e));
       });
     case LIPZ_ACT_SILU:
       return each8(z, [](float v) {
+        v = inside(v);
         const float s = recip<FAST>(1.f + exp_of<FAST>(-v));
         return s * fmaf(v, 1.f - s, 1.f);
       });

@@ -105,3 +105,30 @@ def test_activations_and_slopes_keep_their_tails(act, dtype):
     zd = pre[0, 0].double().cpu()
     _, d, _, terms = act_and_slope(act, zd)
     close(db[0], d, "f32", tol(zd, terms), "slope")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("act", ["linear", "relu", "lrelu", "tanh", "gelu", "silu"])
+def test_activations_and_slopes_at_infinity_are_their_limits(act, dtype):
+    """Such as a pre-activation past the type's range, which is stored as an infinity.  NaN stays NaN."""
+    dt, code = TYPES[dtype][:2]
+    inf, nan = float("inf"), float("nan")
+    far = 60000.0
+    z = torch.tensor([inf, -inf, nan, far, -far], device="cuda")
+    x, w = torch.zeros(1, 1, 1, device="cuda", dtype=dt), torch.ones(1, 1, 5, device="cuda", dtype=dt)
+    y, pre = torch.empty(1, 1, 5, device="cuda", dtype=dt), torch.empty(1, 1, 5, device="cuda", dtype=dt)
+    call("lipz_linear", L.lipz_linear_args(
+        dtype=code, cells=1, rows=1, fan_in=1, fan_out=5, act=CODE[act], slope=0.25, x=mat(x), w=mat(w), pre=mat(pre),
+        y=mat(y), bias=z.data_ptr(), bias_cell=5))
+    db, dy = torch.empty(1, 5, device="cuda"), torch.ones(1, 1, 5, device="cuda", dtype=dt)
+    call("lipz_linear_backward", L.lipz_linear_backward_args(
+        dtype=code, cells=1, rows=1, fan_in=1, fan_out=5, act=CODE[act], slope=0.25, pre=mat(pre), dy=mat(dy),
+        db=db.data_ptr(), db_cell=5))
+    f = torch.tensor(far, device="cuda").to(dt).item()
+    up = {"tanh": (1, 1)}.get(act, (inf, f))
+    low = {"tanh": (-1, -1), "linear": (-inf, -f), "lrelu": (-inf, -f / 4)}.get(act, (0, 0))
+    got = y[0, 0].float().tolist()
+    assert math.isnan(got[2]) and got[:2] + got[3:] == [up[0], low[0], up[1], low[1]]
+    above, below = (0 if act == "tanh" else 1), {"linear": 1, "lrelu": 0.25}.get(act, 0)
+    got = db[0].tolist()
+    assert got[:2] + got[3:] == [above, below] * 2 and (math.isnan(got[2]) or act == "linear")
