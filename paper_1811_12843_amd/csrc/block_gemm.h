@@ -110,9 +110,14 @@ __device__ __forceinline__ void finish8(const Finish& f, int c, int m, int n, in
                                         const f32x8& ws, typename Vec8<T>::type residual) {
   constexpr bool FAST = sizeof(T) < 4;
   if (f.xs) {
-    const float xs = as_global(f.xs)[c * f.xs_cell + m];
+    // significands first, exponents last: the scales' own product may lie below or
+    // above fp32's range where theirs with the sum does not
+    const float xs = as_global(f.xs)[c * f.xs_cell + m], xm = __builtin_amdgcn_frexp_mantf(xs);
+    const int xe = __builtin_amdgcn_frexp_expf(xs);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= xs * ws[e];
+    for (int e = 0; e < 8; ++e)
+      v[e] = __builtin_amdgcn_ldexpf(v[e] * (xm * __builtin_amdgcn_frexp_mantf(ws[e])),
+                                     xe + __builtin_amdgcn_frexp_expf(ws[e]));
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += bias[e];

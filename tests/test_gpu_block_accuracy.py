@@ -132,3 +132,34 @@ def test_activations_and_slopes_at_infinity_are_their_limits(act, dtype):
     above, below = (0 if act == "tanh" else 1), {"linear": 1, "lrelu": 0.25}.get(act, 0)
     got = db[0].tolist()
     assert got[:2] + got[3:] == [above, below] * 2 and (math.isnan(got[2]) or act == "linear")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [3, 40, 2000])  # (64 x 64 tiles with split and whole sums, 128 x 128 tiles)
+def test_e4m3_scales_whose_product_leaves_the_range(rows, dtype):
+    """z = x_scale w_scale sum, where x_scale w_scale alone is subnormal, 0 or infinite in fp32 and z is not; and sums of
+    0 and scales of NaN."""
+    dt, code = TYPES[dtype][:2]
+    K, N = 1100, 1720
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    for up in (False, True):
+        size = 2.0 ** -5 if up else 100.0
+        x, w = ((torch.randn(1, n, K, generator=g, device="cuda") * size).to(F8) for n in (rows, N))
+        x[0, 1] = 0
+        xs, ws = (1 + torch.rand(1, n, generator=g, device="cuda") for n in (rows, N))
+        # sums near 2^18 (2^-5): z between 2^-120 and 2^-110 (2^105 and 2^125)
+        xs, ws = xs * (2.0 ** 66 if up else 2.0 ** -70), ws * (2.0 ** 64 if up else 2.0 ** -62)
+        xs[0, 0], ws[0, 0] = (xs[0, 0] * 2.0 ** -80, ws[0, 0] * 2.0 ** 40) if up else (2.0 ** -126, ws[0, 0])
+        xs[0, 2], ws[0, 5] = float("nan"), float("nan")
+        y, ok = blank(1, rows, N, dt, 3)
+        print(f"[case] e4m3 scales {dtype} rows={rows} up={up}", flush=True)
+        call("lipz_linear_fp8", L.lipz_linear_fp8_args(
+            y_dtype=code, cells=1, rows=rows, fan_in=K, fan_out=N, x=mat(x), w=mat(w), y=mat(y), x_scale=xs.data_ptr(),
+            x_scale_cell=rows, w_scale=ws.data_ptr(), w_scale_cell=N))
+        wt, s = w.double().mT.contiguous(), xs.double()[:, :, None] * ws.double()[:, None]
+        z, terms = torch.bmm(x.double(), wt) * s, torch.bmm(x.double().abs(), wt.abs()) * s
+        far = torch.isinf(z.to(dt))  # past the type's range: an infinity
+        z[far] = z[far] * float("inf")
+        # (the sums' own tolerance, and a subnormal unit where z is that small)
+        close(y, z, dtype, torch.nan_to_num(2.0 ** -23 * (16 + 2 * math.sqrt(K)) * terms) + 2.0 ** -149, "y")
+        assert ok()
