@@ -402,7 +402,8 @@ lipz_status lipz_gemm_timing(lipz_grid* g, double* h_ms, int64_t* h_launches, do
  * Calls check their arguments on the host, enqueue and return; they neither
  * allocate nor synchronise, and may be captured into a graph.  Results do not
  * depend on what else runs: sums are taken in a fixed order.  rows = 0 is
- * allowed (gradients of parameters are then 0).  Errors: LIPZ_E_INVAL,
+ * allowed (gradients of parameters are then 0); what has no element then, the
+ * matrices and vectors of rows, may be NULL.  Errors: LIPZ_E_INVAL,
  * LIPZ_E_WORKSPACE, LIPZ_E_UNSUPPORTED (sizes beyond the limits named at the
  * call) before anything is enqueued, LIPZ_E_HIP. */
 enum { LIPZ_F32 = 0, LIPZ_BF16 = 1, LIPZ_F16 = 2, LIPZ_FP8 = 3 };

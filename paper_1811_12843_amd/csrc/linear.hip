@@ -83,7 +83,7 @@ lipz_status check_linear(const lipz_linear_args* a) {
     return LIPZ_E_INVAL;
   lipz_status st = check_sizes(a->cells, a->rows, a->fan_in, a->fan_out);
   if (st) return st;
-  if (!a->x.p || !a->w.p || !a->y.p) return LIPZ_E_INVAL;
+  if (!a->w.p || (a->rows && (!a->x.p || !a->y.p))) return LIPZ_E_INVAL;
   const int C = a->cells, M = a->rows, K = a->fan_in, N = a->fan_out;
   if ((st = check_mat(a->x, C, M, K, a->dtype, false))) return st;
   if ((st = check_mat(a->w, C, K, N, a->dtype, false))) return st;
@@ -100,9 +100,9 @@ lipz_status check_linear_bwd(const lipz_linear_backward_args* a) {
   lipz_status st = check_sizes(a->cells, a->rows, a->fan_in, a->fan_out);
   if (st) return st;
   const int C = a->cells, M = a->rows, K = a->fan_in, N = a->fan_out;
-  if (!a->dx.p && !a->dw.p && !a->db) return LIPZ_E_INVAL;
-  if (!a->dy.p || (a->act != LIPZ_ACT_LINEAR && !a->pre.p) || (a->dx.p && !a->w.p) || (a->dw.p && !a->x.p))
-    return LIPZ_E_INVAL;
+  if (M && !a->dx.p && !a->dw.p && !a->db) return LIPZ_E_INVAL;
+  if (M && (!a->dy.p || (a->act != LIPZ_ACT_LINEAR && !a->pre.p) || (a->dw.p && !a->x.p))) return LIPZ_E_INVAL;
+  if (a->dx.p && !a->w.p) return LIPZ_E_INVAL;
   if ((st = check_mat(a->dy, C, M, N, a->dtype, false))) return st;
   if (a->act != LIPZ_ACT_LINEAR && (st = check_mat(a->pre, C, M, N, a->dtype, false))) return st;
   if (a->dx.p && ((st = check_mat(a->w, C, K, N, a->dtype, false)) || (st = check_mat(a->dx, C, M, K, a->dtype, true))))

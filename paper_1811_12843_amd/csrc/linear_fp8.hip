@@ -125,7 +125,7 @@ lipz_status check_linear_fp8(const lipz_linear_fp8_args* a) {
     return LIPZ_E_INVAL;
   lipz_status st = check_sizes(a->cells, a->rows, a->fan_in, a->fan_out);
   if (st) return st;
-  if (!a->x.p || !a->w.p || !a->y.p || !a->x_scale || !a->w_scale) return LIPZ_E_INVAL;
+  if (!a->w.p || !a->w_scale || (a->rows && (!a->x.p || !a->y.p || !a->x_scale))) return LIPZ_E_INVAL;
   const int C = a->cells, M = a->rows, K = a->fan_in, N = a->fan_out;
   if ((st = check_mat(a->x, C, M, K, LIPZ_FP8, false))) return st;
   if ((st = check_mat(a->w, C, N, K, LIPZ_FP8, false))) return st;

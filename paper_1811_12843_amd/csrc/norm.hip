@@ -451,7 +451,7 @@ lipz_status check_norm(const lipz_rms_norm_args* a) {
   if (!valid_float(a->dtype) || (a->y_dtype != a->dtype && a->y_dtype != LIPZ_FP8)) return LIPZ_E_INVAL;
   if (a->cells < 1 || a->rows < 0 || a->cols < 1 || !(a->eps > 0.f) || !(a->eps < __builtin_inff())) return LIPZ_E_INVAL;
   if (a->cells > kMaxCells || a->rows > kMaxNormRows || a->cols > kMaxWide) return LIPZ_E_UNSUPPORTED;
-  if (!a->x.p || !a->y.p || !a->gamma || (a->y_dtype == LIPZ_FP8 && !a->y_scale)) return LIPZ_E_INVAL;
+  if (!a->gamma || (a->rows && (!a->x.p || !a->y.p || (a->y_dtype == LIPZ_FP8 && !a->y_scale)))) return LIPZ_E_INVAL;
   lipz_status st;
   if ((st = check_mat(a->x, a->cells, a->rows, a->cols, a->dtype, false))) return st;
   if (a->residual.p && (st = check_mat(a->residual, a->cells, a->rows, a->cols, a->dtype, false))) return st;
@@ -466,7 +466,7 @@ lipz_status check_norm_bwd(const lipz_rms_norm_backward_args* a) {
   if (!a || a->abi_version != LIPZ_ABI_VERSION || !valid_float(a->dtype)) return LIPZ_E_INVAL;
   if (a->cells < 1 || a->rows < 0 || a->cols < 1) return LIPZ_E_INVAL;
   if (a->cells > kMaxCells || a->rows > kMaxNormRows || a->cols > kMaxWide) return LIPZ_E_UNSUPPORTED;
-  if (!a->h.p || !a->dy.p || !a->dx.p || !a->gamma || !a->rstd || (uintptr_t)a->rstd % 4) return LIPZ_E_INVAL;
+  if (!a->gamma || (a->rows && (!a->h.p || !a->dy.p || !a->dx.p || !a->rstd)) || (uintptr_t)a->rstd % 4) return LIPZ_E_INVAL;
   lipz_status st;
   if ((st = check_mat(a->h, a->cells, a->rows, a->cols, a->dtype, false))) return st;
   if ((st = check_mat(a->dy, a->cells, a->rows, a->cols, a->dtype, false))) return st;
