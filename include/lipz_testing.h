@@ -114,6 +114,16 @@ lipz_status lipz_test_es_select(void* hip_stream, const float* d_fit, const floa
  */
 lipz_status lipz_test_tile_map(int32_t n_groups, const int32_t* first_tile, int32_t n_blocks, int32_t* tiles);
 
+/*
+ * Host-only: how a product of lipz_linear, lipz_linear_backward or
+ * lipz_linear_fp8 is cut up: outputs [rows][cols] of each cell, sums of k
+ * products, operands of `dtype`.  *tile = the tile's rows and columns (64, 128
+ * or 256), *splits = the parts of a sum.  LIPZ_E_INVAL or LIPZ_E_UNSUPPORTED
+ * on sizes that the calls refuse.
+ */
+lipz_status lipz_test_product_plan(int32_t dtype, int32_t rows, int32_t cols, int32_t k, int32_t cells, int32_t* tile,
+                                   int32_t* splits);
+
 #ifdef __cplusplus
 }
 #endif

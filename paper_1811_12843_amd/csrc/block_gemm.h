@@ -709,14 +709,47 @@ struct Plan {
 };
 
 inline int tiles_of(int n, int b) { return (n + b - 1) / b; }
+inline int tile_size(int tile) { return tile == TILE_L ? 256 : tile == TILE_M ? 128 : 64; }
 
-// large: whether there is a 256 x 256 kernel.
-inline Plan plan_gemm(int es, int M, int N, int K, int cells, bool large) {
-  Plan p{TILE_S, 1, 0, 0};
-  const int64_t l = (int64_t)tiles_of(M, 256) * tiles_of(N, 256) * cells, m = (int64_t)tiles_of(M, 128) * tiles_of(N, 128) * cells;
-  if (large && l >= 192) p.tile = TILE_L;
-  else if (m >= 192) p.tile = TILE_M;
-  const int b = p.tile == TILE_L ? 256 : p.tile == TILE_M ? 128 : 64;
+// What a wave of 256 tiles takes, one to a compute unit, in microseconds: fixed (the
+// pipeline's fill, the finish) and per 2048 bytes of a row of k.  Fits, to a tenth, of
+// 256 .. 8192 x 4096 outputs at k = 64 .. 4096, each tile alone on all of them; e.g.
+// 8192 x 4096, k = 4096 (16 bits 392, 334, 225 us; fp32 2054, 2201; e4m3 293, 304) and
+// k = 64 (48, 58, 37; 90, 114; 56, 73).
+struct TileTime {
+  double fixed, per_2k;
+};
+inline const TileTime* tile_times(int es) {
+  static constexpr TileTime k32[] = {{1.5, 7.85}, {8, 33.3}}, k16[] = {{0.9, 2.75}, {6, 8.8}, {15, 24}},
+                            k8[] = {{1.1, 4.05}, {8, 14.7}};
+  return es == 4 ? k32 : es == 2 ? k16 : k8;
+}
+
+// The tile whose whole waves take the least time by the table; of times within a
+// tenth the larger tile's, which reads its operands less often.  16 bits, 64 / 128 /
+// 256: 48 cells of 300 x 260, k = 1032 27 / 33 / 38 us (taken: 64), 32 cells of 130 x
+// 2048, k = 512 31 / 45 / 28 (256), 1000 x 4096, k = 4096 59 / 43 / 92 (128).  fp32: 32
+// cells of 10 x 2048, k = 512 51 / 79 (64), 16 of 100 x 2048, k = 1024 92 / 80 (128).
+// e4m3: 8192 x 4096, k = 8192 584 / 530 (128), 2500 x 2000, k = 2048 30 / 47 (64).  Not
+// seen by it: few rows bound by their weights' bytes, 16 cells of 64 x 4096, k = 1024
+// bf16 35 / 38 / 31 (64).
+inline int choose_tile(int es, int M, int N, int K, int cells) {
+  const TileTime* times = tile_times(es);
+  int tile = TILE_S;
+  double best = 0;
+  for (int t = TILE_S; t <= (es == 2 ? TILE_L : TILE_M); ++t) {
+    const int64_t tiles = (int64_t)tiles_of(M, tile_size(t)) * tiles_of(N, tile_size(t)) * cells;
+    const double us = (double)((tiles + 255) / 256) * (times[t].fixed + times[t].per_2k * ((double)K * es / 2048));
+    // (a grid has less than 2^32 threads)
+    if (t == TILE_S || us < 1.1 * best || (tile == TILE_S && tiles > 1 << 21)) tile = t;
+    if (t == TILE_S || us < best) best = us;
+  }
+  return tile;
+}
+
+inline Plan plan_gemm(int es, int M, int N, int K, int cells) {
+  Plan p{choose_tile(es, M, N, K, cells), 1, 0, 0};
+  const int b = tile_size(p.tile);
   const int64_t tiles = (int64_t)tiles_of(M, b) * tiles_of(N, b) * cells;
   const int slices = tiles_of(K * es, p.tile == TILE_L ? 64 : 128);
   int splits = 1;
@@ -733,7 +766,7 @@ inline Plan plan_gemm(int es, int M, int N, int K, int cells, bool large) {
 
 template <class E, class T, bool AKC, bool BKC>
 inline void launch_gemm(GemmArgs& P, const Plan& plan, hipStream_t s) {
-  const int b = plan.tile == TILE_L ? 256 : plan.tile == TILE_M ? 128 : 64;
+  const int b = tile_size(plan.tile);
   P.tiles_m = tiles_of(P.M, b);
   P.tiles_n = tiles_of(P.N, b);
   P.splits = plan.splits;

@@ -131,7 +131,7 @@ FwdLayout fwd_layout(const lipz_linear_args* a) {
   w.pack_w = !loads_as_is(a->w, N, es, false);
   if (w.pack_x) w.x = b.take(packed_bytes(M, K, es, C));
   if (w.pack_w) w.w = b.take(packed_bytes(K, N, es, C));
-  w.plan = plan_gemm(es, M, N, K, C, es < 4);
+  w.plan = plan_gemm(es, M, N, K, C);
   w.sums = b.take(w.plan.part_bytes);
   w.total = b.at + 256;
   return w;
@@ -179,8 +179,8 @@ BwdLayout bwd_layout(const lipz_linear_backward_args* a) {
   if (w.pack_x) w.x = b.take(packed_bytes(M, K, es, C));
   if (w.pack_w) w.w = b.take(packed_bytes(K, N, es, C));
   if (a->db) w.part = b.take((size_t)C * w.chunks * N * 4);
-  w.dx = plan_gemm(es, M, K, N, C, es < 4);
-  w.dw = plan_gemm(es, K, N, M, C, es < 4);
+  w.dx = plan_gemm(es, M, K, N, C);
+  w.dw = plan_gemm(es, K, N, M, C);
   const size_t x = a->dx.p ? w.dx.part_bytes : 0, d = a->dw.p ? w.dw.part_bytes : 0;
   w.sums = b.take(x > d ? x : d);
   w.total = b.at + 256;

@@ -161,7 +161,7 @@ Fp8Layout fp8_layout(const lipz_linear_fp8_args* a) {
   w.pack_w = !loads_as_is(a->w, K, 1, true);
   if (w.pack_x) w.x = b.take(packed_bytes(M, K, 1, C));
   if (w.pack_w) w.w = b.take(packed_bytes(N, K, 1, C));
-  w.plan = plan_gemm(1, M, N, K, C, false);
+  w.plan = plan_gemm(1, M, N, K, C);
   w.sums = b.take(w.plan.part_bytes);
   w.total = b.at + 256;
   return w;

@@ -1,6 +1,7 @@
-// Test hook of include/lipz_testing.h: one grouped-GEMM problem.
+// Test hooks of include/lipz_testing.h.
 #include <string.h>
 
+#include "block_gemm.h"
 #include "lipz_internal.h"
 #include "lipz_testing.h"
 
@@ -117,5 +118,17 @@ extern "C" lipz_status lipz_test_tile_map(int32_t n_groups, const int32_t* first
     grp.first_tile[g] = first_tile[g];
   }
   for (int32_t b = 0; b < n_blocks; ++b) tiles[b] = lipz::xcd_group_tile(b, n_blocks, grp);
+  return LIPZ_OK;
+}
+
+extern "C" lipz_status lipz_test_product_plan(int32_t dtype, int32_t rows, int32_t cols, int32_t k, int32_t cells,
+                                              int32_t* tile, int32_t* splits) {
+  if (!tile || !splits || rows < 1 || (dtype != LIPZ_FP8 && !valid_float(dtype))) return LIPZ_E_INVAL;
+  lipz_status st = check_sizes(cells, rows, k, cols);
+  if (st || (st = check_tiles(rows, cols, cells))) return st;
+  const int es = elem_size(dtype);
+  const Plan p = plan_gemm(es, rows, cols, k, cells);
+  *tile = tile_size(p.tile);
+  *splits = p.splits;
   return LIPZ_OK;
 }

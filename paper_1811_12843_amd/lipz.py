@@ -162,6 +162,7 @@ _SIGS = {
                               _i32]),
     "lipz_test_es_select": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _i64, _i64, _f32]),
     "lipz_test_tile_map": (_i32, [_i32, _vp, _i32, _vp]),
+    "lipz_test_product_plan": (_i32, [_i32] * 5 + [ctypes.POINTER(_i32)] * 2),
 }
 
 for _n, _c in _BLOCK.items():
@@ -420,3 +421,11 @@ def lipz_test_tile_map(first_tile, n_blocks):
     out = (_i32 * n_blocks)()
     _check(load_library().lipz_test_tile_map(len(first_tile), ft, n_blocks, out), "lipz_test_tile_map")
     return list(out)
+
+
+def lipz_test_product_plan(dtype, rows, cols, k, cells=1):
+    """(tile, splits) of a product of the residual-block operators (host only)."""
+    tile, splits = _i32(), _i32()
+    _check(load_library().lipz_test_product_plan(dtype, rows, cols, k, cells, ctypes.byref(tile), ctypes.byref(splits)),
+           "lipz_test_product_plan")
+    return tile.value, splits.value
