@@ -251,18 +251,6 @@ __device__ __forceinline__ f32x8 slope8(int act, f32x8 z, float slope) {
   }
 }
 
-// ---- sums over the lanes of a wave, in a fixed order ----
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) v += __shfl_xor(v, s, 64);
-  return v;
-}
-__device__ __forceinline__ float wave_max_nan(float v) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) v = max_nan(v, __shfl_xor(v, s, 64));
-  return v;
-}
-
 // ---- the host's checks ----
 
 constexpr int64_t kMaxWide = 1 << 20;  // columns of a matrix

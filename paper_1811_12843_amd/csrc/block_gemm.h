@@ -58,10 +58,8 @@ struct Fp8 {};
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_any;
 typedef __attribute__((address_space(3))) char lds_char;
-typedef __attribute__((address_space(3))) float lds_float;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 template <class V>
 __device__ __forceinline__ V lds_get(const lds_char* p) {
@@ -137,14 +135,12 @@ __device__ __forceinline__ f32x8 column8(const float* p, int64_t cell, int c, in
 // ---- operands ----
 
 // The place of chunk x (16 bytes) of k row k in a KM tile of R columns is
-// x ^ km_swizzle(k); MF: the MFMA's rows.  16 bits: a transposing read of a
-// group of 16 lanes takes 32 bytes of each of four k rows; two groups are
-// served at a time: other k rows, 8 on (MF = 16), or the next 32 bytes of the
-// same (MF = 32).  fp32: a read takes 64 bytes of k rows 4 g + u.
-template <int ES, int R, int MF>
+// x ^ km_swizzle(k).  16 bits: a transposing read of a group of 16 lanes takes 32
+// bytes of each of four k rows; two groups, 8 k rows apart, are served at a time.
+// fp32: a read takes 64 bytes of k rows 4 g + u.
+template <int ES, int R>
 __device__ __forceinline__ int km_swizzle(int k) {
   if (ES == 4) return 4 * ((k >> 2) & 3);
-  if (MF == 32) return 4 * (k & 3);
   if (R * ES >= 256) return 2 * ((k & 3) | ((k >> 1) & 4));
   return 2 * (((k >> 1) & 1) | ((k >> 2) & 2));
 }
@@ -183,7 +179,7 @@ struct Operand {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int q = i * NT + (int)threadIdx.x, row = q / CPR, at = q % CPR;
-      const int x = at ^ (KC ? kc_swizzle<SB>(row) : km_swizzle<ES, R, Tile::MF>(row));
+      const int x = at ^ (KC ? kc_swizzle<SB>(row) : km_swizzle<ES, R>(row));
       off[i] = (uint32_t)row * (uint32_t)ld + x * 16;
       if (KC) k = x * EPC;
     }
@@ -210,7 +206,7 @@ struct Operand {
 // row l % 16 and, of the slice's half kk, 16 bytes of k (16 bits: k = 32 kk +
 // 8 (l / 16) .. + 7; fp32: 16 kk + 4 (l / 16) .. + 3; e4m3: 64 kk + 16 (l / 16) .. +
 // 15; A and B need only agree).  N of them, 16 rows apart.
-template <int ES, bool KC, int R, int MF, int SB, int N>
+template <int ES, bool KC, int R, int SB, int N>
 struct Fragments {
   static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
     const int li = lane & 15, g = lane >> 4;
@@ -221,7 +217,7 @@ struct Fragments {
         out[i] = lds_get<u32x4>(st + r * SB + (((4 * kk + g) ^ kc_swizzle<SB>(li)) << 4));
       } else {  // fp32
         const int k = 16 * kk + 4 * g;
-        const lds_char* p = st + k * (R * 4) + (((r >> 2) ^ km_swizzle<4, R, 16>(k)) << 4) + 4 * (r & 3);
+        const lds_char* p = st + k * (R * 4) + (((r >> 2) ^ km_swizzle<4, R>(k)) << 4) + 4 * (r & 3);
 #pragma unroll
         for (int u = 0; u < 4; ++u) out[i][u] = lds_get<uint32_t>(p + u * (R * 4));
       }
@@ -247,39 +243,15 @@ __device__ __forceinline__ int hidden(int v) {
   return v;
 }
 template <int R, int SB, int N>
-struct Fragments<2, false, R, 16, SB, N> {
+struct Fragments<2, false, R, SB, N> {
   static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
     const int li = lane & 15, k = 8 * (lane >> 4) + (li >> 2);
     const int p = k * (R * 2) + 8 * (li & 1), p4 = hidden(p + 4 * R * 2);
-    const int x = (r0 >> 3) + ((li >> 1) & 1), w = km_swizzle<2, R, 16>(k);
+    const int x = (r0 >> 3) + ((li >> 1) & 1), w = km_swizzle<2, R>(k);
 #pragma unroll
     for (int i = 0; i < N; ++i)
       out[i] = read_transposed(st, p + (((x + 2 * i) ^ w) << 4) + kk * 32 * R * 2,
                                p4 + (((x + 2 * i) ^ w) << 4) + kk * 32 * R * 2);
-  }
-};
-
-// For 32 x 32 MFMAs, slices of 64 bytes: lane l holds row l % 32, k = 16 kk +
-// 8 (l / 32) .. + 7 (16 bits).
-template <int ES, int R, int N>
-struct Fragments<ES, true, R, 32, 64, N> {
-  static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
-    const int li = lane & 31, g = lane >> 5;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      out[i] = lds_get<u32x4>(st + (r0 + 32 * i + li) * 64 + (((2 * kk + g) ^ kc_swizzle<64>(li)) << 4));
-  }
-};
-template <int R, int N>
-struct Fragments<2, false, R, 32, 64, N> {
-  static __device__ __forceinline__ void read(const lds_char* st, int r0, int kk, int lane, u32x4* out) {
-    const int li = lane & 15, k = 8 * (lane >> 5) + (li >> 2);
-    const int p = k * (R * 2) + 8 * (li & 1), p4 = hidden(p + 4 * R * 2);
-    const int x = (r0 >> 3) + 2 * ((lane >> 4) & 1) + ((li >> 1) & 1), w = km_swizzle<2, R, 32>(k);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      out[i] = read_transposed(st, p + (((x + 4 * i) ^ w) << 4) + kk * 16 * R * 2,
-                               p4 + (((x + 4 * i) ^ w) << 4) + kk * 16 * R * 2);
   }
 };
 
@@ -290,17 +262,11 @@ struct Mma<__bf16> {
   static __device__ __forceinline__ f32x4 run(u32x4 b, u32x4 a, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
   }
-  static __device__ __forceinline__ f32x16 run(u32x4 b, u32x4 a, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
-  }
 };
 template <>
 struct Mma<_Float16> {
   static __device__ __forceinline__ f32x4 run(u32x4 b, u32x4 a, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ f32x16 run(u32x4 b, u32x4 a, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
   }
 };
 template <>
@@ -315,23 +281,22 @@ struct Mma<float> {
 
 // ---- tiles ----
 
-template <int BM_, int BN_, int WM_, int WN_, int NS_, int SB_, int MF_>
+template <int BM_, int BN_, int WM_, int WN_, int NS_, int SB_>
 struct TileShape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;  // WM x WN waves
-  static constexpr int NS = NS_, SB = SB_, MF = MF_;            // LDS stages, bytes of a slice's row, MFMA's rows
+  static constexpr int NS = NS_, SB = SB_;                      // LDS stages, bytes of a slice's row
   static constexpr int NT = 64 * WM * WN, TM = BM / WM, TN = BN / WN;
-  static constexpr int MI = TM / MF, NI = TN / MF;
+  static constexpr int MI = TM / 16, NI = TN / 16;              // MFMAs of 16 x 16
   static constexpr int A_BYTES = BM * SB, B_BYTES = BN * SB;
   static constexpr int LOADS = (A_BYTES + B_BYTES) / 16 / NT;  // of a slice, per wave
   static_assert(NS >= 2 && NS <= 4 && 2 * NS >= WM * WN && TM % 32 == 0 && TN % 32 == 0 && BM * SB >= 4096);
-  typedef std::conditional_t<MF == 16, f32x4, f32x16> Acc;
 };
 // (three stages: three workgroups to a compute unit; with four, two of them, one row of
 // 4096 x 4096 bf16 13.2 us instead of 12.3, gradients at 1999 x 1201 x 777 f16 44.5
 // instead of 43.4)
-typedef TileShape<64, 64, 2, 2, 3, 128, 16> TileS;
-typedef TileShape<128, 128, 2, 2, 4, 128, 16> TileM;
-typedef TileShape<256, 256, 2, 4, 4, 64, 16> TileL;
+typedef TileShape<64, 64, 2, 2, 3, 128> TileS;
+typedef TileShape<128, 128, 2, 2, 4, 128> TileM;
+typedef TileShape<256, 256, 2, 4, 4, 64> TileL;
 
 // Waits until all but this wave's last n vector loads have landed and its LDS
 // accesses are done, then for the other waves.  No more than that: the
@@ -356,11 +321,11 @@ struct Parts {
   }
   template <int P>
   __device__ __forceinline__ void read(const lds_char* sa, const lds_char* sb, int wm, int wn, int lane) {
-    if (P == 0) Fragments<ES, BKC, Tile::BN, Tile::MF, Tile::SB, Tile::NI>::read(sb, wn, 0, lane, b[0]);
-    Fragments<ES, AKC, Tile::BM, Tile::MF, Tile::SB, H>::read(sa, wm + Tile::MF * H * P, 0, lane, a[P]);
+    if (P == 0) Fragments<ES, BKC, Tile::BN, Tile::SB, Tile::NI>::read(sb, wn, 0, lane, b[0]);
+    Fragments<ES, AKC, Tile::BM, Tile::SB, H>::read(sa, wm + 16 * H * P, 0, lane, a[P]);
   }
   template <int P>
-  __device__ __forceinline__ void mma(typename Tile::Acc (&acc)[Tile::MI][Tile::NI]) {
+  __device__ __forceinline__ void mma(f32x4 (&acc)[Tile::MI][Tile::NI]) {
 #pragma unroll
     for (int i = 0; i < H; ++i)
 #pragma unroll
@@ -378,11 +343,11 @@ struct Parts<E, AKC, BKC, Tile, false> {
   __device__ __forceinline__ void turn() {}
   template <int P>
   __device__ __forceinline__ void read(const lds_char* sa, const lds_char* sb, int wm, int wn, int lane) {
-    Fragments<ES, BKC, Tile::BN, Tile::MF, Tile::SB, Tile::NI>::read(sb, wn, P, lane, f[P].b);
-    Fragments<ES, AKC, Tile::BM, Tile::MF, Tile::SB, Tile::MI>::read(sa, wm, P, lane, f[P].a);
+    Fragments<ES, BKC, Tile::BN, Tile::SB, Tile::NI>::read(sb, wn, P, lane, f[P].b);
+    Fragments<ES, AKC, Tile::BM, Tile::SB, Tile::MI>::read(sa, wm, P, lane, f[P].a);
   }
   template <int P>
-  __device__ __forceinline__ void mma(typename Tile::Acc (&acc)[Tile::MI][Tile::NI]) {
+  __device__ __forceinline__ void mma(f32x4 (&acc)[Tile::MI][Tile::NI]) {
 #pragma unroll
     for (int i = 0; i < Tile::MI; ++i)
 #pragma unroll
@@ -405,12 +370,12 @@ struct Parts<Fp8, AKC, BKC, Tile, false> {
   __device__ __forceinline__ void read(const lds_char* sa, const lds_char* sb, int wm, int wn, int lane) {
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      if (P == 0) Fragments<1, true, Tile::BN, Tile::MF, Tile::SB, Tile::NI>::read(sb, wn, kk, lane, fb[0][kk]);
-      Fragments<1, true, Tile::BM, Tile::MF, Tile::SB, H>::read(sa, wm + Tile::MF * H * P, kk, lane, fa[P][kk]);
+      if (P == 0) Fragments<1, true, Tile::BN, Tile::SB, Tile::NI>::read(sb, wn, kk, lane, fb[0][kk]);
+      Fragments<1, true, Tile::BM, Tile::SB, H>::read(sa, wm + 16 * H * P, kk, lane, fa[P][kk]);
     }
   }
   template <int P>
-  __device__ __forceinline__ void mma(typename Tile::Acc (&acc)[Tile::MI][Tile::NI]) {
+  __device__ __forceinline__ void mma(f32x4 (&acc)[Tile::MI][Tile::NI]) {
     const auto& a = fa[P];
     const auto& b = fb[P];
 #pragma unroll
@@ -496,8 +461,8 @@ __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) 
   load(stage1);
   if constexpr (NS > 2) load(stage2);
   if constexpr (NS > 3) load(stage3);
-  typename Tile::Acc acc[Tile::MI][Tile::NI] = {};
-  Parts<E, AKC, BKC, Tile, ES == 2 && Tile::MF == 16 && Tile::SB == 64> F;
+  f32x4 acc[Tile::MI][Tile::NI] = {};
+  Parts<E, AKC, BKC, Tile, ES == 2 && Tile::SB == 64> F;
   // Keeps the order that is written, where registers allow it (both operands
   // across k take more addresses): 6 cold 8192 x 4096 x 4096 products along k
   // 1383 us, 1475 in the compiler's order.
@@ -562,20 +527,12 @@ __global__ __launch_bounds__(Tile::NT) void block_gemm_kernel(const GemmArgs P) 
 #pragma unroll
     for (int bi = 0; bi < Tile::TM / 32; ++bi) {
       const int row = lane >> 2, m = m0 + 32 * bi + row;
-      // C of a 16 x 16 MFMA: lane l holds row l % 16, columns 4 (l / 16) .. + 3; of a
-      // 32 x 32 one: row l % 32, columns 8 q + 4 (l / 32) .. + 3, q = 0 .. 3
+      // C of a 16 x 16 MFMA: lane l holds row l % 16, columns 4 (l / 16) .. + 3
       auto put = [&](int at, int x, f32x4 v) { *(lds_f32x4*)(mine + at * 128 + ((x ^ (at & 7)) << 4)) = v; };
-      if constexpr (Tile::MF == 16) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) put(16 * i + (lane & 15), 4 * j + (lane >> 4), acc[2 * bi + i][2 * bj + j]);
-      } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          put(lane & 31, 2 * q + (lane >> 5),
-              f32x4{acc[bi][bj][4 * q], acc[bi][bj][4 * q + 1], acc[bi][bj][4 * q + 2], acc[bi][bj][4 * q + 3]});
-      }
+        for (int j = 0; j < 2; ++j) put(16 * i + (lane & 15), 4 * j + (lane >> 4), acc[2 * bi + i][2 * bj + j]);
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
