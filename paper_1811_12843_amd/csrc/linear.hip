@@ -110,7 +110,7 @@ lipz_status check_linear_bwd(const lipz_linear_backward_args* a) {
   if (a->dw.p && ((st = check_mat(a->x, C, M, K, a->dtype, false)) || (st = check_mat(a->dw, C, K, N, a->dtype, true))))
     return st;
   if (a->db && (st = check_vec(a->db, a->db_cell, C, N, true))) return st;
-  if ((st = check_tiles(M, K, C)) || (st = check_tiles(K, N, C))) return st;
+  if ((a->dx.p && (st = check_tiles(M, K, C))) || (a->dw.p && (st = check_tiles(K, N, C)))) return st;
   return check_tiles(M, N, C);
 }
 
