@@ -141,7 +141,8 @@ constexpr float kFp8MinScale = 1.17549435e-38f;  // 2^-126: its reciprocal and t
 // max that keeps a NaN of either side
 __device__ __forceinline__ float max_nan(float a, float b) { return (a > b || a != a) ? a : b; }
 // The scale of a row of largest magnitude m >= 0, infinite or NaN: NaN for the
-// last two.  m times the fp32 reciprocal: m / scale may then be 448 and one
+// last two.  m times the fp32 reciprocal, as torch divides a tensor by a number, so
+// that values quantised there agree to the bit; m / scale may then be 448 and one
 // unit in fp32's last place, which still rounds to 448.
 __device__ __forceinline__ float fp8_scale(float m) {
   const float s = m * (1.f / kFp8Max);

@@ -36,10 +36,12 @@
 // Large products are bound by the matrix cores' rate at the clock that the
 // card's power leaves and by the finish, whose memory traffic overlaps no other
 // tile's products (the stages take 128 KiB of LDS, so a compute unit holds one
-// workgroup): 8192 x 4096 x 8192 bf16 with GELU, residual and pre 525 us (1.05
-// PFLOP/s, matrix cores 49 % busy); with the finish as a loop over the wave's
-// columns 563 us.  e4m3 8192 x 8192 x 4096 with the weights' quantisation 590 us.
-// One row: the weights' bytes, 4096 x 4096 bf16 12.3 us, 7 of them the product.
+// workgroup): 8192 x 4096 x 8192 bf16 with GELU, residual and pre 534 us (1.03
+// PFLOP/s, matrix cores 48 % busy), of them 455 without residual and pre and with
+// SiLU; with the finish as a loop over the wave's columns 40 us more.  e4m3 8192 x
+// 8192 x 4096 with the weights' quantisation 597 us (matrix cores 40 % busy, beside
+// the conversion of every fragment in every wave).
+// One row: the weights' bytes, 4096 x 4096 bf16 12.5 us, 7 of them the product.
 #pragma once
 
 #include "block.h"
@@ -47,13 +49,13 @@
 namespace lipz {
 
 // The operand type of e4m3 products.  Their fragments are turned into f16, which
-// holds every e4m3 value, and multiplied at fp32 accuracy.  The e4m3 MFMAs, at up to
-// twice the rate, align their products to the largest of their k before they add
-// them, so that one large product takes the low bits of all others: sums of 1024
-// with a 448 x 448 of either sign in every 64 terms and remainders between 1 and 4
-// came out up to 8.7e-5 of the sum of magnitudes and 12 % of their value off (in f16:
-// below 1e-7 and 2.4e-4).  That costs 590 us instead of 307 at 8192 x 8192 x 4096, and
-// 13.0 instead of 11.7 at 8 x 4096 x 8192.
+// holds every e4m3 value, and multiplied at fp32 accuracy.  The scaled e4m3 MFMA, at
+// twice the rate, aligns its products to the largest of them before it adds them,
+// so that one large product takes the low bits of all others: sums of 1024 with a
+// 448 x 448 of either sign in every 64 terms and remainders between 1 and 4 came out
+// up to 8.7e-5 of the sum of magnitudes and 12 % of their value off (in f16 exact).
+// That costs 597 us instead of 307 at 8192 x 8192 x 4096 with the weights'
+// quantisation, and 12.4 instead of 11.7 at 8 x 4096 x 8192.
 struct Fp8 {};
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));

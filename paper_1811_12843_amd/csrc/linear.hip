@@ -2,11 +2,13 @@
 // and residual in the epilogue, and their gradients (kernel: block_gemm.h).
 //
 // Backward: one pass forms dz = dy act'(pre), rounds it to the operands' type
-// for the two products (which take it from L2 or the Infinity Cache), and
-// sums its columns, unrounded, per 32 rows; a second adds those for db.  dx =
+// for the two products (matrix cores take no wider operand beside a 16-bit one,
+// and fp32 products run at a seventh of the rate; large bf16 gradients are then
+// 2.3e-3 off in the 2-norm instead of their own rounding's 1.7e-3), which take it
+// from L2 or the Infinity Cache, and sums its columns, unrounded, per 32 rows; a second adds those for db.  dx =
 // dz w^T reads both operands along k; dw = x^T dz both across it.
-// At 8192 x 4096 x 4096 bf16, 488 us together: dz 35 to 42 us (201 MB, 4.8 TB/s and
-// more), the products 244 and 212 us (1.1 and 1.3 PFLOP/s).
+// At 8192 x 4096 x 4096 bf16, 488 to 500 us together: dz 38 to 44 us (201 MB, 4.6
+// TB/s and more), the products 249 and 215 us (1.1 and 1.3 PFLOP/s).
 #include "block_gemm.h"
 
 namespace lipz {

@@ -8,14 +8,15 @@
 // rows of the group, the columns' sums of dy h rstd; a block adds its groups'
 // in LDS and a second kernel the blocks', each in a fixed order.
 //
-// TPR is the smallest of 8 .. 64 lanes of a wave, 256 or 1024 threads that holds
-// a row with at most NV = 4 accesses per lane, so short rows share a wave and
-// long ones spread over a block; rows over 32768 columns (16384 in the backward
+// TPR lanes with NV accesses each hold a row: up to 512 columns the fewest of 8 ..
+// 64 lanes with one access, so that short rows share a wave; up to 2048 a wave with
+// two or four; up to 8192 a block of 256 threads, then one of 1024, with two or
+// four; rows over 32768 columns (16384 in the backward
 // pass, which keeps more of a row) are read again for each of their passes
 // instead.
 //
 // Bound by memory, each input read once: 16384 x 4096 bf16 with residual 94 us
-// (5.7 TB/s; a large copy runs at 4.8), gradients of 8192 x 8192 bf16 107 us (5.0
+// (5.7 TB/s; a large copy runs at 4.8), gradients of 8192 x 8192 bf16 108 us (5.0
 // TB/s, 6 us of it the columns' sums); one row of 4096 to e4m3 6.6 us, a launch.
 #include "block.h"
 
